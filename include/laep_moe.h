@@ -68,6 +68,8 @@ extern "C" {
 #define LAEP_CALL_FFN_FWD 2
 #define LAEP_CALL_FFN_BWD 3
 #define LAEP_CALL_ROUTE_BWD 4
+#define LAEP_CALL_LAYER_NORM_BWD 5 /* laep_block.h; (T, 1, 1, d_model, 0) */
+#define LAEP_CALL_BALANCE 6        /* laep_block.h; (T, n_seq, E, 0, 0)   */
 
 /* Limits of the library. */
 #define LAEP_MAX_EXPERTS 256

@@ -15,10 +15,12 @@ moe       router, top-k gating, expert histogram and offsets, permute,
 laep      the LAEP prune rule (Section 3.2, Eqs. (1)-(2); Appendix,
           Algorithm 1) and expert rearrangement (Section 3.3; Appendix,
           Algorithm 2)
+block     layer norm, balance loss and 8-bit activation checkpoints around
+          the layer, and their backward
 
 Pins (tests marked ``not gpu``) tie every function to something other than
 itself: brute-force enumeration, invariants, closed forms, finite
 differences, an independent autograd evaluation and hand-worked examples.
 Functions without such a pin say "parity unpinned" in their docstring.
 """
-from . import numerics, moe, laep  # noqa: F401
+from . import numerics, moe, laep, block  # noqa: F401

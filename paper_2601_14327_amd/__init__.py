@@ -18,12 +18,22 @@ Expert Pruning acts on), each a call into hand-written gfx950 HIP kernels:
     moe_combine_bwd, moe_grouped_ffn_bwd, moe_permute_bwd   backward
     moe_route_bwd        router / gate backward (softmax Jacobian, dW_r, dx)
     laep_rearrange       host utility: balanced expert placement
+
+and what a pre-norm MoE block computes around them:
+
+    moe_layer_norm, moe_layer_norm_bwd      residual add and layer norm, gradients
+    moe_balance_loss, moe_balance_loss_bwd  balance loss per batch or sequence, expert
+                         counts, the logits' gradient
+    moe_act8_save, moe_act8_load            activations kept in 8 bits
+    moe_swiglu_bwd_act8  the SwiGLU backward at them
+
     laep_calib_copy, laep_calib_read,  measurement calls (attained peaks,
     laep_calib_mfma                    the router's feed bound)
     laep_ffn_fwd_row_tile              which kernels a forward call runs
 """
 from ._lib import (  # noqa: F401
-    LAEP_BF16, LAEP_CALL_FFN_BWD, LAEP_CALL_FFN_FWD, LAEP_F32, LaepError, LIB_PATH, lib)
+    LAEP_ACT8_BLOCK, LAEP_BF16, LAEP_CALL_BALANCE, LAEP_CALL_FFN_BWD, LAEP_CALL_FFN_FWD,
+    LAEP_CALL_LAYER_NORM_BWD, LAEP_F32, LaepError, LIB_PATH, lib)
 from .api import (  # noqa: F401
     ffn_bwd_ws_views,
     ffn_fwd_h_view,
@@ -36,6 +46,10 @@ from .api import (  # noqa: F401
     laep_prune_mask,
     laep_rearrange,
     laep_repack_experts,
+    moe_act8_load,
+    moe_act8_save,
+    moe_balance_loss,
+    moe_balance_loss_bwd,
     moe_combine,
     moe_combine_bwd,
     moe_expert_counts,
@@ -44,12 +58,15 @@ from .api import (  # noqa: F401
     moe_grouped_ffn_fwd,
     moe_grouped_ffn_fwd_gather,
     moe_grouped_ffn_fwd_gather_combine,
+    moe_layer_norm,
+    moe_layer_norm_bwd,
     moe_permute,
     moe_permute_bwd,
     moe_route,
     moe_route_bwd,
     moe_route_count,
     moe_route_count_noalloc,
+    moe_swiglu_bwd_act8,
     workspace_bytes,
 )
 from .layer import MoELayerPlan, layer_forward  # noqa: F401

@@ -1,4 +1,4 @@
-"""ctypes loader of liblaep_moe.so and the C signatures (include/laep_moe.h).
+"""ctypes loader of liblaep_moe.so and the C signatures (include/*.h).
 
 The library is loaded from the package directory only.  If it has not been
 built, every call raises -- there is no fallback implementation.
@@ -20,6 +20,10 @@ LAEP_CALL_COUNTS = 1
 LAEP_CALL_FFN_FWD = 2
 LAEP_CALL_FFN_BWD = 3
 LAEP_CALL_ROUTE_BWD = 4
+LAEP_CALL_LAYER_NORM_BWD = 5
+LAEP_CALL_BALANCE = 6
+
+LAEP_ACT8_BLOCK = 32    # columns that share a scale of an 8-bit checkpoint
 
 ERROR_NAMES = {
     1: "LAEP_ERR_INVALID_ARG",
@@ -43,6 +47,7 @@ _p = ctypes.c_void_p
 _i = ctypes.c_int
 _i64 = ctypes.c_int64
 _sz = ctypes.c_size_t
+_f = ctypes.c_float
 _d = ctypes.c_double
 
 # name -> (restype, argtypes)
@@ -76,6 +81,14 @@ SIGNATURES = {
     "moe_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
     "laep_rearrange": (_i, [_p, _i, _i, _p, _p, _p]),
     "laep_last_error": (ctypes.c_char_p, []),
+    # the block around the experts (laep_block.h)
+    "moe_layer_norm": (_i, [_p, _p, _p, _p, _i, _i, _i, _f, _p, _p, _p, _p, _p]),
+    "moe_layer_norm_bwd": (_i, [_p, _p, _p, _p, _p, _p, _i, _i, _i, _p, _p, _p, _p, _sz, _p]),
+    "moe_balance_loss": (_i, [_p, _p, _p, _p, _i, _i, _i, _i, _f, _p, _p, _p, _p, _p, _sz, _p]),
+    "moe_balance_loss_bwd": (_i, [_p, _p, _p, _p, _p, _i, _i, _i, _p, _i, _p]),
+    "moe_act8_save": (_i, [_p, _i, _i64, _i, _p, _p, _p]),
+    "moe_act8_load": (_i, [_p, _p, _i, _i64, _i, _p, _p]),
+    "moe_swiglu_bwd_act8": (_i, [_p, _p, _p, _i, _i64, _i, _p, _p, _p]),
     # measurement calls (laep_calib.h)
     "laep_calib_copy": (_i, [_p, _p, _sz, _p]),
     "laep_calib_mfma": (_i, [_i, _i, _p, _p]),

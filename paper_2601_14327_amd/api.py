@@ -13,7 +13,8 @@ from typing import Optional, Tuple
 
 import torch
 
-from ._lib import (LAEP_BF16, LAEP_CALL_COUNTS, LAEP_CALL_FFN_BWD, LAEP_CALL_FFN_FWD,
+from ._lib import (LAEP_ACT8_BLOCK, LAEP_BF16, LAEP_CALL_BALANCE, LAEP_CALL_COUNTS,
+                   LAEP_CALL_FFN_BWD, LAEP_CALL_FFN_FWD, LAEP_CALL_LAYER_NORM_BWD,
                    LAEP_CALL_ROUTE_BWD, LAEP_F32, LaepError, check, lib)
 
 _DT = {torch.float32: LAEP_F32, torch.bfloat16: LAEP_BF16}
@@ -522,6 +523,177 @@ def laep_rearrange(loads, n_groups: int):
     check(lib().laep_rearrange(loads.ctypes.data, n, n_groups, group_of.ctypes.data,
                                order.ctypes.data, sums.ctypes.data))
     return dict(group_of=group_of, order=order, sums=sums[:n_groups])
+
+
+# ---- the block around the experts (laep_block.h) ---------------------------------------
+def _want(t: Optional[torch.Tensor], name: str, shape, dtype) -> Optional[torch.Tensor]:
+    """A given device tensor of this shape and dtype (None passes)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    return _dev(t, name)
+
+
+def _out(t: Optional[torch.Tensor], name: str, shape, dtype, device) -> torch.Tensor:
+    """The given output buffer, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    return _want(t, name, shape, dtype)
+
+
+def moe_layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: Optional[torch.Tensor] = None, *,
+                   residual=None, eps: float = 1e-5, out=None, sum_out=None, mean=None,
+                   rstd=None):
+    """Residual add and layer norm of the rows of x [T, d]; gamma and beta are
+    float32 [d].  Returns (y, s, mean, rstd): s = x + residual as stored (x
+    itself without a residual), the row statistics float32 [T].  ``sum_out``
+    may be x or residual."""
+    _dev(x, "x")
+    T, d = x.shape
+    dev = x.device
+    _want(gamma, "gamma", (d,), torch.float32), _want(beta, "beta", (d,), torch.float32)
+    _want(residual, "residual", (T, d), x.dtype)
+    code = _dtype_code(x)
+    y = _out(out, "out", (T, d), x.dtype, dev)
+    if residual is not None or sum_out is not None:   # the C call refuses one without the other
+        sum_out = _out(sum_out, "sum_out", (T, d), x.dtype, dev)
+    mean = _out(mean, "mean", (T,), torch.float32, dev)
+    rstd = _out(rstd, "rstd", (T,), torch.float32, dev)
+    check(lib().moe_layer_norm(_ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), code, T, d,
+                               float(eps), _ptr(sum_out), _ptr(y), _ptr(mean), _ptr(rstd),
+                               _stream(dev)))
+    return y, (x if sum_out is None else sum_out), mean, rstd
+
+
+def moe_layer_norm_bwd(dy: torch.Tensor, s: torch.Tensor, gamma: torch.Tensor,
+                       mean: torch.Tensor, rstd: torch.Tensor, *, dres=None,
+                       weights: bool = True, want_dbeta: bool = True, dx=None, dgamma=None,
+                       dbeta=None, ws=None):
+    """Backward of moe_layer_norm: s, mean and rstd as it returned them, ``dres``
+    [T, d] the gradient that reaches s past the norm.  ``weights=False`` skips
+    dgamma and dbeta.  ``dx`` may be dy or dres.  Returns (dx, dgamma, dbeta),
+    None for what was not computed."""
+    _dev(s, "s")
+    T, d = s.shape
+    dev = s.device
+    f32 = torch.float32
+    _want(dy, "dy", (T, d), s.dtype), _want(dres, "dres", (T, d), s.dtype)
+    _want(gamma, "gamma", (d,), f32)
+    _want(mean, "mean", (T,), f32), _want(rstd, "rstd", (T,), f32)
+    code = _dtype_code(s)
+    dx = _out(dx, "dx", (T, d), s.dtype, dev)
+    dgamma = _out(dgamma, "dgamma", (d,), f32, dev) if weights else None
+    dbeta = _out(dbeta, "dbeta", (d,), f32, dev) if weights and want_dbeta else None
+    ws = _workspace(ws, workspace_bytes(LAEP_CALL_LAYER_NORM_BWD, T, 1, 1, d) if weights else 0,
+                    dev)
+    check(lib().moe_layer_norm_bwd(_ptr(dy), _ptr(s), _ptr(gamma), _ptr(mean), _ptr(rstd),
+                                   _ptr(dres), code, T, d, _ptr(dx), _ptr(dgamma), _ptr(dbeta),
+                                   _ptr(ws), ws.numel() * ws.element_size(), _stream(dev)))
+    return dx, dgamma, dbeta
+
+
+def _sequences(seq_offsets) -> int:
+    if seq_offsets is None:
+        return 1
+    if seq_offsets.dtype != torch.int32 or seq_offsets.dim() != 1 or seq_offsets.numel() < 2:
+        raise ValueError("seq_offsets must be an int32 tensor [n_seq + 1]")
+    _dev(seq_offsets, "seq_offsets")
+    return seq_offsets.numel() - 1
+
+
+def moe_balance_loss(logits: torch.Tensor, topk_idx: torch.Tensor, *, coef: float = 1.0,
+                     alive=None, seq_offsets=None, loss=None, counts=None, prob_mean=None,
+                     grad_coef=None, ws=None):
+    """Balance loss of the router's float32 logits [T, E] and its selection
+    topk_idx [T, k], over the batch or per sequence (``seq_offsets`` int32
+    [n_seq + 1] on the device).  Returns (loss [1], counts [n_seq, E] int32,
+    prob_mean [n_seq, E], grad_coef [n_seq, E]); grad_coef goes to
+    moe_balance_loss_bwd or moe_route_bwd_balance."""
+    _dev(logits, "logits")
+    T, E = logits.shape
+    k = topk_idx.shape[1]
+    dev = logits.device
+    f32 = torch.float32
+    _want(logits, "logits", (T, E), f32), _want(topk_idx, "topk_idx", (T, k), torch.int32)
+    _want(alive, "alive", (E,), torch.uint8)
+    S = _sequences(seq_offsets)
+    loss = _out(loss, "loss", (1,), f32, dev)
+    counts = _out(counts, "counts", (S, E), torch.int32, dev)
+    prob_mean = _out(prob_mean, "prob_mean", (S, E), f32, dev)
+    grad_coef = _out(grad_coef, "grad_coef", (S, E), f32, dev)
+    ws = _workspace(ws, workspace_bytes(LAEP_CALL_BALANCE, T, S, E), dev)
+    check(lib().moe_balance_loss(_ptr(logits), _ptr(topk_idx), _ptr(alive), _ptr(seq_offsets), T,
+                                 E, k, S, float(coef), _ptr(loss), _ptr(counts), _ptr(prob_mean),
+                                 _ptr(grad_coef), _ptr(ws), ws.numel() * ws.element_size(),
+                                 _stream(dev)))
+    return loss, counts, prob_mean, grad_coef
+
+
+def moe_balance_loss_bwd(logits: torch.Tensor, grad_coef: torch.Tensor, *, dloss=None,
+                         alive=None, seq_offsets=None, dlogits=None, accumulate: bool = False):
+    """Gradient of the balance loss with respect to the logits, the counts held
+    fixed; ``dloss`` is a float32 device tensor of one element (None: 1).
+    ``accumulate`` adds to the given dlogits."""
+    _dev(logits, "logits")
+    T, E = logits.shape
+    S = _sequences(seq_offsets)
+    f32 = torch.float32
+    _want(logits, "logits", (T, E), f32), _want(grad_coef, "grad_coef", (S, E), f32)
+    _want(alive, "alive", (E,), torch.uint8)
+    if dloss is not None and (dloss.dtype != f32 or dloss.numel() != 1 or not dloss.is_cuda):
+        raise ValueError("dloss must be a float32 device tensor of one element")
+    if accumulate and dlogits is None:
+        raise ValueError("accumulate needs dlogits")
+    dlogits = _out(dlogits, "dlogits", (T, E), f32, logits.device)
+    check(lib().moe_balance_loss_bwd(_ptr(logits), _ptr(grad_coef), _ptr(alive),
+                                     _ptr(seq_offsets), _ptr(dloss), T, E, S, _ptr(dlogits),
+                                     int(accumulate), _stream(logits.device)))
+    return dlogits
+
+
+def moe_act8_save(act: torch.Tensor, *, q=None, scale=None):
+    """act [R, C] (C a multiple of 32) in 8 bits with one power-of-two scale per
+    32 columns of a row.  Returns (q [R, C] int8, scale [R, C/32] uint8, the
+    scale's biased exponent)."""
+    _dev(act, "act")
+    R, C = act.shape
+    q = _out(q, "q", (R, C), torch.int8, act.device)
+    scale = _out(scale, "scale", (R, C // LAEP_ACT8_BLOCK), torch.uint8, act.device)
+    check(lib().moe_act8_save(_ptr(act), _dtype_code(act), R, C, _ptr(q), _ptr(scale),
+                              _stream(act.device)))
+    return q, scale
+
+
+def moe_act8_load(q: torch.Tensor, scale: torch.Tensor, dtype: torch.dtype = torch.bfloat16, *,
+                  out=None):
+    """The values an 8-bit checkpoint stands for, in dtype (exact in bfloat16)."""
+    _dev(q, "q")
+    R, C = q.shape
+    _want(q, "q", (R, C), torch.int8)
+    _want(scale, "scale", (R, C // LAEP_ACT8_BLOCK), torch.uint8)
+    if dtype not in _DT:
+        raise LaepError(2, f"unsupported dtype {dtype}")
+    out = _out(out, "out", (R, C), dtype, q.device)
+    check(lib().moe_act8_load(_ptr(q), _ptr(scale), _DT[dtype], R, C, _ptr(out),
+                              _stream(q.device)))
+    return out
+
+
+def moe_swiglu_bwd_act8(q: torch.Tensor, scale: torch.Tensor, dh: torch.Tensor, *, da=None,
+                        h=None):
+    """SwiGLU backward at pre-activations kept in 8 bits (q [R, 2f], scale
+    [R, 2f/32]) from dh [R, f].  Returns (da [R, 2f], h [R, f]); h is the
+    recomputed input of the down projection and may be dh's buffer."""
+    _dev(dh, "dh")
+    R, f = dh.shape
+    _want(q, "q", (R, 2 * f), torch.int8)
+    _want(scale, "scale", (R, 2 * f // LAEP_ACT8_BLOCK), torch.uint8)
+    da = _out(da, "da", (R, 2 * f), dh.dtype, dh.device)
+    h = _out(h, "h", (R, f), dh.dtype, dh.device)
+    check(lib().moe_swiglu_bwd_act8(_ptr(q), _ptr(scale), _ptr(dh), _dtype_code(dh), R, f,
+                                    _ptr(da), _ptr(h), _stream(dh.device)))
+    return da, h
 
 
 # ---- measurement calls (laep_calib.h) -------------------------------------------------

@@ -9,6 +9,7 @@
 #include <cstring>
 
 #include "../../include/laep_moe.h"
+#include "../../include/laep_block.h"
 #include "../../include/laep_calib.h"
 #include "internal.hpp"
 
@@ -111,6 +112,10 @@ size_t moe_workspace_bytes(int which_call, int T, int k, int E, int d_model, int
       return laep::ffn_bwd_ws_bytes(R, E, d_model, d_ff, laep::kDtypeBf16);
     case LAEP_CALL_ROUTE_BWD:
       return laep::route_bwd_ws_bytes(T, k, E, d_model < 0 ? 0 : d_model);
+    case LAEP_CALL_LAYER_NORM_BWD:
+      return laep::layer_norm_bwd_ws_bytes(T, d_model < 0 ? 0 : d_model);
+    case LAEP_CALL_BALANCE:
+      return laep::balance_ws_bytes(T, E, k);
     default:
       return 0;
   }
@@ -594,6 +599,183 @@ int moe_permute_bwd(const void* dx_perm, const int32_t* dest_row, int T, int k, 
   return hip_status(laep::launch_combine(dx_perm, nullptr, dest_row, T, k, d_model, dtype, dx,
                                          as_stream(stream)),
                     "moe_permute_bwd");
+}
+
+// ---- the block around the experts (laep_block.h) ----------------------------------
+int moe_layer_norm(const void* x, const void* residual, const float* gamma, const float* beta,
+                   int dtype, int T, int d_model, float eps, void* sum_out, void* y, float* mean,
+                   float* rstd, void* stream) {
+  int rc = check_dtype(dtype);
+  if (rc) return rc;
+  if ((rc = check_rows(T, 1, d_model))) return rc;
+  REQUIRE(eps >= 0.0f && std::isfinite(eps), LAEP_ERR_INVALID_ARG,
+          "moe_layer_norm: eps=%g must be finite and >= 0", (double)eps);
+  REQUIRE(residual || !sum_out, LAEP_ERR_INVALID_ARG,
+          "moe_layer_norm: sum_out needs a residual (without one the sum is x)");
+  if (T == 0) return ok();
+  REQUIRE(x && gamma && y, LAEP_ERR_INVALID_ARG,
+          "moe_layer_norm: x, gamma and y must be non-null");
+  REQUIRE(aligned16(x) && aligned16(residual) && aligned16(gamma) && aligned16(beta) &&
+              aligned16(sum_out) && aligned16(y),
+          LAEP_ERR_INVALID_ARG, "moe_layer_norm: buffers must be 16-byte aligned");
+  REQUIRE(y != x && y != residual && y != sum_out, LAEP_ERR_INVALID_ARG,
+          "moe_layer_norm: y must not alias x, residual or sum_out");
+  return hip_status(laep::launch_layer_norm(x, residual, gamma, beta, dtype, T, d_model, eps,
+                                            sum_out, y, mean, rstd, as_stream(stream)),
+                    "moe_layer_norm");
+}
+
+int moe_layer_norm_bwd(const void* dy, const void* s, const float* gamma, const float* mean,
+                       const float* rstd, const void* dres, int dtype, int T, int d_model,
+                       void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
+                       void* stream) {
+  int rc = check_dtype(dtype);
+  if (rc) return rc;
+  if ((rc = check_rows(T, 1, d_model))) return rc;
+  REQUIRE(dgamma || !dbeta, LAEP_ERR_INVALID_ARG,
+          "moe_layer_norm_bwd: dbeta needs dgamma (they are computed together)");
+  REQUIRE(aligned16(dgamma) && aligned16(dbeta), LAEP_ERR_INVALID_ARG,
+          "moe_layer_norm_bwd: dgamma and dbeta must be 16-byte aligned");
+  if (T > 0) {
+    REQUIRE(dy && s && gamma && mean && rstd && dx, LAEP_ERR_INVALID_ARG,
+            "moe_layer_norm_bwd: dy, s, gamma, mean, rstd and dx must be non-null");
+    REQUIRE(aligned16(dy) && aligned16(s) && aligned16(gamma) && aligned16(dres) && aligned16(dx),
+            LAEP_ERR_INVALID_ARG, "moe_layer_norm_bwd: buffers must be 16-byte aligned");
+    REQUIRE(dx != s, LAEP_ERR_INVALID_ARG, "moe_layer_norm_bwd: dx must not alias s");
+    if (dgamma) {
+      const size_t need = laep::layer_norm_bwd_ws_bytes(T, d_model);
+      REQUIRE(ws_bytes >= need, LAEP_ERR_WORKSPACE,
+              "moe_layer_norm_bwd: workspace %zu < %zu bytes", ws_bytes, need);
+      REQUIRE(ws && aligned16(ws), LAEP_ERR_INVALID_ARG,
+              "moe_layer_norm_bwd: ws must be non-null and 16-byte aligned");
+    }
+  }
+  return hip_status(laep::launch_layer_norm_bwd(dy, s, gamma, mean, rstd, dres, dtype, T, d_model,
+                                                dx, dgamma, dbeta, ws, as_stream(stream)),
+                    "moe_layer_norm_bwd");
+}
+
+}  // extern "C"
+
+namespace {
+
+// sequences of the balance loss: offsets, or none for one sequence of all tokens
+int check_sequences(const char* name, const int32_t* seq_offsets, int n_seq) {
+  REQUIRE(n_seq >= 1 && n_seq <= LAEP_MAX_SEQUENCES, LAEP_ERR_INVALID_ARG,
+          "%s: n_seq=%d outside [1, %d]", name, n_seq, LAEP_MAX_SEQUENCES);
+  REQUIRE(seq_offsets || n_seq == 1, LAEP_ERR_INVALID_ARG,
+          "%s: n_seq=%d needs seq_offsets (without them the batch is one sequence)", name, n_seq);
+  return LAEP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int moe_balance_loss(const float* logits, const int32_t* topk_idx, const uint8_t* alive,
+                     const int32_t* seq_offsets, int T, int E, int k, int n_seq, float coef,
+                     float* loss, int32_t* counts, float* prob_mean, float* grad_coef, void* ws,
+                     size_t ws_bytes, void* stream) {
+  int rc = check_experts(E, k);
+  if (rc) return rc;
+  REQUIRE(T >= 0 && (long long)T * k <= 0x7FFFFFFFll, LAEP_ERR_INVALID_ARG,
+          "moe_balance_loss: T=%d is negative or T*k exceeds int32", T);
+  if ((rc = check_sequences("moe_balance_loss", seq_offsets, n_seq))) return rc;
+  REQUIRE(std::isfinite(coef), LAEP_ERR_INVALID_ARG, "moe_balance_loss: coef=%g must be finite",
+          (double)coef);
+  REQUIRE(loss && counts && prob_mean && grad_coef, LAEP_ERR_INVALID_ARG,
+          "moe_balance_loss: loss, counts, prob_mean and grad_coef must be non-null");
+  REQUIRE(T == 0 || (logits && topk_idx), LAEP_ERR_INVALID_ARG,
+          "moe_balance_loss: logits and topk_idx must be non-null");
+  REQUIRE(aligned16(logits), LAEP_ERR_INVALID_ARG,
+          "moe_balance_loss: logits must be 16-byte aligned");
+  const size_t need = laep::balance_ws_bytes(T, E, n_seq);
+  REQUIRE(ws_bytes >= need, LAEP_ERR_WORKSPACE, "moe_balance_loss: workspace %zu < %zu bytes",
+          ws_bytes, need);
+  REQUIRE(ws && aligned16(ws), LAEP_ERR_INVALID_ARG,
+          "moe_balance_loss: ws must be non-null and 16-byte aligned");
+  return hip_status(laep::launch_balance(logits, topk_idx, alive, seq_offsets, T, E, k, n_seq,
+                                         coef, loss, counts, prob_mean, grad_coef, ws,
+                                         as_stream(stream)),
+                    "moe_balance_loss");
+}
+
+int moe_balance_loss_bwd(const float* logits, const float* grad_coef, const uint8_t* alive,
+                         const int32_t* seq_offsets, const float* dloss, int T, int E, int n_seq,
+                         float* dlogits, int accumulate, void* stream) {
+  int rc = check_experts(E, 1);
+  if (rc) return rc;
+  REQUIRE(T >= 0, LAEP_ERR_INVALID_ARG, "T=%d < 0", T);
+  if ((rc = check_sequences("moe_balance_loss_bwd", seq_offsets, n_seq))) return rc;
+  if (T == 0) return ok();
+  REQUIRE(logits && grad_coef && dlogits, LAEP_ERR_INVALID_ARG,
+          "moe_balance_loss_bwd: logits, grad_coef and dlogits must be non-null");
+  REQUIRE(aligned16(logits) && aligned16(grad_coef) && aligned16(dlogits), LAEP_ERR_INVALID_ARG,
+          "moe_balance_loss_bwd: logits, grad_coef and dlogits must be 16-byte aligned");
+  return hip_status(laep::launch_balance_bwd(logits, grad_coef, alive, seq_offsets, dloss, T, E,
+                                             n_seq, dlogits, accumulate != 0, as_stream(stream)),
+                    "moe_balance_loss_bwd");
+}
+
+}  // extern "C"
+
+namespace {
+
+int check_act8(const char* name, int dtype, int64_t R, int C) {
+  int rc = check_dtype(dtype);
+  if (rc) return rc;
+  REQUIRE(R >= 0 && R <= 0x7FFFFFFFll, LAEP_ERR_INVALID_ARG, "%s: R=%lld outside [0, 2^31)", name,
+          (long long)R);
+  REQUIRE(C > 0 && C % LAEP_ACT8_BLOCK == 0, LAEP_ERR_INVALID_ARG,
+          "%s: %d columns are not a positive multiple of %d", name, C, LAEP_ACT8_BLOCK);
+  return LAEP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int moe_act8_save(const void* act, int dtype, int64_t R, int C, int8_t* q, uint8_t* scale,
+                  void* stream) {
+  int rc = check_act8("moe_act8_save", dtype, R, C);
+  if (rc) return rc;
+  if (R == 0) return ok();
+  REQUIRE(act && q && scale, LAEP_ERR_INVALID_ARG,
+          "moe_act8_save: act, q and scale must be non-null");
+  REQUIRE(aligned16(act) && aligned16(q) && aligned16(scale), LAEP_ERR_INVALID_ARG,
+          "moe_act8_save: buffers must be 16-byte aligned");
+  return hip_status(laep::launch_act8_save(act, dtype, R, C, q, scale, as_stream(stream)),
+                    "moe_act8_save");
+}
+
+int moe_act8_load(const int8_t* q, const uint8_t* scale, int dtype, int64_t R, int C, void* act,
+                  void* stream) {
+  int rc = check_act8("moe_act8_load", dtype, R, C);
+  if (rc) return rc;
+  if (R == 0) return ok();
+  REQUIRE(act && q && scale, LAEP_ERR_INVALID_ARG,
+          "moe_act8_load: q, scale and act must be non-null");
+  REQUIRE(aligned16(act) && aligned16(q) && aligned16(scale), LAEP_ERR_INVALID_ARG,
+          "moe_act8_load: buffers must be 16-byte aligned");
+  return hip_status(laep::launch_act8_load(q, scale, dtype, R, C, act, as_stream(stream)),
+                    "moe_act8_load");
+}
+
+int moe_swiglu_bwd_act8(const int8_t* q, const uint8_t* scale, const void* dh, int dtype,
+                        int64_t R, int d_ff, void* da, void* h, void* stream) {
+  int rc = check_act8("moe_swiglu_bwd_act8", dtype, R, d_ff);
+  if (rc) return rc;
+  REQUIRE(d_ff <= 0x3FFFFFFF, LAEP_ERR_INVALID_ARG, "moe_swiglu_bwd_act8: d_ff=%d too large", d_ff);
+  if (R == 0) return ok();
+  REQUIRE(q && scale && dh && da && h, LAEP_ERR_INVALID_ARG,
+          "moe_swiglu_bwd_act8: q, scale, dh, da and h must be non-null");
+  REQUIRE(aligned16(q) && aligned16(scale) && aligned16(dh) && aligned16(da) && aligned16(h),
+          LAEP_ERR_INVALID_ARG, "moe_swiglu_bwd_act8: buffers must be 16-byte aligned");
+  REQUIRE(da != dh && da != h, LAEP_ERR_INVALID_ARG,
+          "moe_swiglu_bwd_act8: da must not alias dh or h");
+  return hip_status(laep::launch_swiglu_bwd_act8(q, scale, dh, dtype, R, d_ff, da, h,
+                                                 as_stream(stream)),
+                    "moe_swiglu_bwd_act8");
 }
 
 // ---- measurement calls (laep_calib.h) --------------------------------------------

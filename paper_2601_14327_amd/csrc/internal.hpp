@@ -130,6 +130,35 @@ hipError_t launch_route_bwd(const float* dgate, const int32_t* idx, const float*
                             float* dw_router, float* dbias, void* dx, int accumulate_dx, void* ws,
                             hipStream_t s);
 
+// Layer norm of the block's rows, and its backward (ws: the partial weight gradients).
+hipError_t launch_layer_norm(const void* x, const void* residual, const float* gamma,
+                             const float* beta, int dtype, int T, int d, float eps, void* sum_out,
+                             void* y, float* mean, float* rstd, hipStream_t s);
+size_t layer_norm_bwd_ws_bytes(int T, int d);
+hipError_t launch_layer_norm_bwd(const void* dy, const void* sv, const float* gamma,
+                                 const float* mean, const float* rstd, const void* dres, int dtype,
+                                 int T, int d, void* dx, float* dgamma, float* dbeta, void* ws,
+                                 hipStream_t s);
+
+// Balance loss of the router.
+size_t balance_ws_bytes(int T, int E, int n_seq);
+hipError_t launch_balance(const float* logits, const int32_t* topk_idx, const uint8_t* alive,
+                          const int32_t* seq_offsets, int T, int E, int k, int n_seq, float coef,
+                          float* loss, int32_t* counts, float* prob_mean, float* grad_coef,
+                          void* ws, hipStream_t s);
+hipError_t launch_balance_bwd(const float* logits, const float* grad_coef, const uint8_t* alive,
+                              const int32_t* seq_offsets, const float* dloss, int T, int E,
+                              int n_seq, float* dlogits, int accumulate, hipStream_t s);
+
+// 8-bit activation checkpoints: q [R, C], scale [R, C / 32].
+hipError_t launch_act8_save(const void* act, int dtype, int64_t R, int C, void* q, uint8_t* scale,
+                            hipStream_t s);
+hipError_t launch_act8_load(const void* q, const uint8_t* scale, int dtype, int64_t R, int C,
+                            void* act, hipStream_t s);
+// (h may be dh)
+hipError_t launch_swiglu_bwd_act8(const void* q, const uint8_t* scale, const void* dh, int dtype,
+                                  int64_t R, int f, void* da, void* h, hipStream_t s);
+
 // Measurement kernels (laep_calib.h).
 hipError_t launch_calib_copy(const void* src, void* dst, size_t bytes, hipStream_t s);
 hipError_t launch_calib_mfma(int n_workgroups, int iters, float* out, hipStream_t s);
