@@ -39,7 +39,9 @@ def _dev(t: torch.Tensor, name: str) -> torch.Tensor:
 
 
 def _stream(device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+    # the current stream's handle without the Stream object around it, whose making
+    # costs 2 us of every call
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def workspace_bytes(which: int, T: int, k: int, E: int, d_model: int = 0, d_ff: int = 0) -> int:
@@ -530,7 +532,7 @@ def _want(t: Optional[torch.Tensor], name: str, shape, dtype) -> Optional[torch.
     """A given device tensor of this shape and dtype (None passes)."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
     return _dev(t, name)
 

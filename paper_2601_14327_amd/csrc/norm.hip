@@ -4,15 +4,387 @@
 // and, with xh = (s - mu) rstd and g = gamma dy,
 //   dx = round(rstd (g - mean_c g - xh mean_c (g xh)) + dres)
 //   dgamma = sum_t dy xh,  dbeta = sum_t dy
-// All are HBM-bound.  The variance is the mean of the centred squares (a second
-// pass over the row), so a large common offset costs no digits.
+// All are HBM-bound.
+#include <type_traits>
+
 #include "common.hpp"
 #include "internal.hpp"
 
 namespace laep {
 namespace {
 
-constexpr int kNormThreads = 256;
+// 8 consecutive elements in their storage format
+template <typename T> struct Vec8;
+template <> struct Vec8<bf16_t> {
+  u32x4_t r;
+  __device__ __forceinline__ void load(const bf16_t* p) {
+    r = ld_stream(reinterpret_cast<const u32x4_t*>(p));
+  }
+  __device__ __forceinline__ void get(float v[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = lo_bf16(r[i]);
+      v[2 * i + 1] = hi_bf16(r[i]);
+    }
+  }
+  // v rounded to storage, and widened again
+  __device__ __forceinline__ void put(float v[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    get(v);
+  }
+  __device__ __forceinline__ void store(bf16_t* p) const {
+    st_stream(reinterpret_cast<u32x4_t*>(p), r);
+  }
+};
+template <> struct Vec8<float> {
+  f32x4_t a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = ld_stream(reinterpret_cast<const f32x4_t*>(p));
+    b = ld_stream(reinterpret_cast<const f32x4_t*>(p) + 1);
+  }
+  __device__ __forceinline__ void get(float v[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] = a[i];
+      v[4 + i] = b[i];
+    }
+  }
+  __device__ __forceinline__ void put(float v[8]) {
+    a = f32x4_t{v[0], v[1], v[2], v[3]};
+    b = f32x4_t{v[4], v[5], v[6], v[7]};
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    st_stream(reinterpret_cast<f32x4_t*>(p), a);
+    st_stream(reinterpret_cast<f32x4_t*>(p) + 1, b);
+  }
+};
+
+// A row belongs to NL lanes (a power of two), lane l holding the 8-column vectors
+// l, l + NL, ... (VPL of them), so it is read once; a workgroup of at least kFwdThreads
+// or kBwdThreads threads walks the rows, gamma, beta and, backwards, its columns' sums
+// staying in registers.  One vector a lane wherever 512 lanes hold the row: with two,
+// four or eight the forward took 210, 212 and 226 us against 195 at 32768 x 4096 bf16
+// with a residual.  Forward: 1024 workgroups of 256 threads, each row's loads issued
+// after the last one's stores: 179 us (6.0 TB/s of 6.2 that a copy reaches), 25 us at
+// 8192 x 2048; loading the next row ahead 196 and 29 us, a workgroup for every row 205
+// and 26.  Backward: 256 workgroups of 512 threads, since each writes a row of partial
+// sums, with the next row's loads ahead: 184 us (5.8 TB/s) at 32768 x 4096 with dres,
+// 30 us at 8192 x 2048; 256 threads 186 and 41, 512 workgroups 189 and 34.
+constexpr int kFwdThreads = 256, kBwdThreads = 512, kMaxLanes = 512;
+template <int NL, int MIN_NT> struct NormShape {
+  static constexpr int NT = NL > MIN_NT ? NL : MIN_NT;
+  static constexpr int ROWS = NT / NL;                   // rows at a time
+  static constexpr int WAVES = NL > kWave ? NL / kWave : 1;  // waves of a row
+};
+
+// sum over the row's lanes inside a wave
+template <int NL>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int off = (NL < kWave ? NL : kWave) / 2; off >= 1; off >>= 1) v += __shfl_xor(v, off, kWave);
+  return v;
+}
+
+template <typename T, int NL, int VPL>
+__global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_kernel(
+    const T* x, const T* residual, const float* __restrict__ gamma,
+    const float* __restrict__ beta, unsigned n_rows, int d, float eps, T* sum_out, T* __restrict__ y,
+    float* __restrict__ mean, float* __restrict__ rstd) {
+  using S = NormShape<NL, kFwdThreads>;
+  __shared__ float s_red[2][S::NT / kWave][2];
+  const int nvec = d / 8;
+  const int l = threadIdx.x % NL, sub = threadIdx.x / NL;
+  const int wave = threadIdx.x / kWave, wave0 = wave - wave % S::WAVES;
+  float g[VPL][8], b[VPL][8];
+  int cols = 0;               // columns of this wave's part of a row
+#pragma unroll
+  for (int u = 0; u < VPL; ++u) {
+    const int v = l + u * NL;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) g[u][q] = b[u][q] = 0.0f;
+    if (v < nvec) {
+      Elem<float>::load8(gamma + (size_t)v * 8, g[u]);
+      if (beta) Elem<float>::load8(beta + (size_t)v * 8, b[u]);
+    }
+    if (NL > kWave) cols += 8 * min(kWave, max(0, nvec - u * NL - (wave % S::WAVES) * kWave));
+  }
+  if (NL <= kWave) cols = d;
+  Vec8<T> xv[VPL], rv[VPL];
+  auto load = [&](unsigned row) {
+#pragma unroll
+    for (int u = 0; u < VPL; ++u) {
+      const int v = l + u * NL;
+      if (row < n_rows && v < nvec) {
+        xv[u].load(x + (size_t)row * d + (size_t)v * 8);
+        if (residual) rv[u].load(residual + (size_t)row * d + (size_t)v * 8);
+      }
+    }
+  };
+  const unsigned step = gridDim.x * S::ROWS;
+  unsigned row = blockIdx.x * S::ROWS + sub;
+  unsigned base = blockIdx.x * S::ROWS;   // < n_rows; rows and steps may pass int32
+  for (int it = 0;; it ^= 1) {
+    const bool more = n_rows - base > step;
+    load(row);
+    float s[VPL][8];
+    float sum = 0.0f;
+#pragma unroll
+    for (int u = 0; u < VPL; ++u) {
+      const int v = l + u * NL;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) s[u][q] = 0.0f;
+      if (row >= n_rows || v >= nvec) continue;
+      xv[u].get(s[u]);
+      if (residual) {
+        float r[8];
+        rv[u].get(r);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s[u][q] += r[q];
+        xv[u].put(s[u]);
+        if (sum_out) xv[u].store(sum_out + (size_t)row * d + (size_t)v * 8);
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q) sum += s[u][q];
+    }
+    // the wave's own mean and centred squares; several waves' are merged by
+    //   M2 = sum_w (M2_w + n_w (mu_w - mu)^2)
+    float mu = cols ? lanes_sum<NL>(sum) / (float)cols : 0.0f;
+    float sq = 0.0f;
+#pragma unroll
+    for (int u = 0; u < VPL; ++u)
+      if (l + u * NL < nvec) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sq += (s[u][q] - mu) * (s[u][q] - mu);
+      }
+    sq = lanes_sum<NL>(sq);
+    if constexpr (S::WAVES > 1) {
+      if (threadIdx.x % kWave == 0) {
+        s_red[it][wave][0] = mu;
+        s_red[it][wave][1] = sq;
+      }
+      __syncthreads();
+      float tot = 0.0f;
+      int n[S::WAVES];
+#pragma unroll
+      for (int w = 0; w < S::WAVES; ++w) {
+        n[w] = 0;
+#pragma unroll
+        for (int u = 0; u < VPL; ++u) n[w] += 8 * min(kWave, max(0, nvec - u * NL - w * kWave));
+        tot += s_red[it][wave0 + w][0] * (float)n[w];
+      }
+      mu = tot / (float)d;
+      sq = 0.0f;
+#pragma unroll
+      for (int w = 0; w < S::WAVES; ++w) {
+        const float off = s_red[it][wave0 + w][0] - mu;
+        sq += s_red[it][wave0 + w][1] + (float)n[w] * off * off;
+      }
+    }
+    const float rs = 1.0f / sqrtf(sq / (float)d + eps);
+    if (row < n_rows) {
+#pragma unroll
+      for (int u = 0; u < VPL; ++u) {
+        const int v = l + u * NL;
+        if (v >= nvec) continue;
+        float o[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) o[q] = (s[u][q] - mu) * rs * g[u][q] + b[u][q];
+        Vec8<T> ov;
+        ov.put(o);
+        ov.store(y + (size_t)row * d + (size_t)v * 8);
+      }
+      if (l == 0) {
+        if (mean) mean[row] = mu;
+        if (rstd) rstd[row] = rs;
+      }
+    }
+    if (!more) break;
+    base += step;
+    row += step;
+  }
+}
+
+// dx of the rows a workgroup walks, and its rows' sums of dy xh and dy.
+template <typename T, int NL, int VPL>
+__global__ __launch_bounds__((NormShape<NL, kBwdThreads>::NT)) void norm_bwd_kernel(
+    const T* dy, const T* __restrict__ sv, const float* __restrict__ gamma,
+    const float* __restrict__ mean, const float* __restrict__ rstd, const T* dres,
+    unsigned n_rows, int d, T* dx, float* __restrict__ part) {
+  using S = NormShape<NL, kBwdThreads>;
+  // four vectors a lane leave no registers for the next row, nor for gamma
+  constexpr bool AHEAD = VPL <= 2;
+  __shared__ float s_red[2][S::NT / kWave][2];
+  const int nvec = d / 8;
+  const int l = threadIdx.x % NL, sub = threadIdx.x / NL;
+  const int wave = threadIdx.x / kWave, wave0 = wave - wave % S::WAVES;
+  float held[AHEAD ? VPL : 1][8], wg[VPL][8], wb[VPL][8];
+#pragma unroll
+  for (int u = 0; u < VPL; ++u) {
+    const int v = l + u * NL;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) wg[u][q] = wb[u][q] = 0.0f;
+    if (AHEAD && v < nvec) Elem<float>::load8(gamma + (size_t)v * 8, held[AHEAD ? u : 0]);
+  }
+  auto gamma_of = [&](int u, float g[8]) {   // of a vector inside the row
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) g[q] = held[u][q];
+    } else {
+      Elem<float>::load8(gamma + (size_t)(l + u * NL) * 8, g);
+    }
+  };
+  Vec8<T> xv[VPL], yv[VPL], rv[VPL];
+  float mu = 0.0f, rs = 0.0f;
+  auto load = [&](unsigned row) {
+    if (row < n_rows) {
+      mu = mean[row];
+      rs = rstd[row];
+    }
+#pragma unroll
+    for (int u = 0; u < VPL; ++u) {
+      const int v = l + u * NL;
+      const size_t at = (size_t)row * d + (size_t)v * 8;
+      if (row < n_rows && v < nvec) {
+        xv[u].load(sv + at);
+        yv[u].load(dy + at);
+        if (dres) rv[u].load(dres + at);
+      }
+    }
+  };
+  const unsigned step = gridDim.x * S::ROWS;
+  unsigned row = blockIdx.x * S::ROWS + sub;
+  if constexpr (AHEAD) load(row);
+  unsigned base = blockIdx.x * S::ROWS;   // < n_rows; rows and steps may pass int32
+  for (int it = 0;; it ^= 1) {
+    const bool more = n_rows - base > step;
+    if constexpr (!AHEAD) load(row);
+    const bool on = row < n_rows;
+    const float r1 = rs;
+    float xh[VPL][8], dv[VPL][8];
+    Vec8<T> res[VPL];
+    float a = 0.0f, b = 0.0f;
+#pragma unroll
+    for (int u = 0; u < VPL; ++u) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) xh[u][q] = dv[u][q] = 0.0f;
+      if (!on || l + u * NL >= nvec) continue;
+      xv[u].get(xh[u]);
+      yv[u].get(dv[u]);
+      if (AHEAD && dres) res[u] = rv[u];
+      float g[8];
+      gamma_of(u, g);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        xh[u][q] = (xh[u][q] - mu) * r1;
+        a += g[q] * dv[u][q];
+        b += g[q] * dv[u][q] * xh[u][q];
+        wg[u][q] += dv[u][q] * xh[u][q];
+        wb[u][q] += dv[u][q];
+      }
+    }
+    if (AHEAD && more) load(row + step);
+    a = lanes_sum<NL>(a);
+    b = lanes_sum<NL>(b);
+    if constexpr (S::WAVES > 1) {
+      if (threadIdx.x % kWave == 0) {
+        s_red[it][wave][0] = a;
+        s_red[it][wave][1] = b;
+      }
+      __syncthreads();
+      a = b = 0.0f;
+#pragma unroll
+      for (int w = 0; w < S::WAVES; ++w) {
+        a += s_red[it][wave0 + w][0];
+        b += s_red[it][wave0 + w][1];
+      }
+    }
+    a /= (float)d;
+    b /= (float)d;
+#pragma unroll
+    for (int u = 0; u < VPL; ++u) {
+      const int v = l + u * NL;
+      if (!on || v >= nvec) continue;
+      float o[8], r[8], g[8];
+      gamma_of(u, g);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) o[q] = r1 * (g[q] * dv[u][q] - a - xh[u][q] * b);
+      if (dres) {
+        (AHEAD ? res[u] : rv[u]).get(r);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) o[q] += r[q];
+      }
+      Vec8<T> ov;
+      ov.put(o);
+      ov.store(dx + (size_t)row * d + (size_t)v * 8);
+    }
+    if (!more) break;
+    base += step;
+    row += step;
+  }
+  if (!part) return;
+  // rows side by side in the workgroup: their sums added in order through LDS
+  float* const out = part + (size_t)blockIdx.x * 2 * d;
+  __shared__ float s_sum[S::ROWS > 1 ? S::ROWS * NL * 8 : 1];
+#pragma unroll
+  for (int u = 0; u < VPL; ++u)
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      const float* const w = which ? wb[u] : wg[u];
+      const int v = l + u * NL;
+      if constexpr (S::ROWS == 1) {
+        if (v < nvec) Elem<float>::store8(out + which * d + (size_t)v * 8, w);
+      } else {
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s_sum[(sub * NL + l) * 8 + q] = w[q];
+        __syncthreads();
+        for (int c = threadIdx.x; c < NL * 8; c += S::NT) {
+          float t = 0.0f;
+#pragma unroll
+          for (int i = 0; i < S::ROWS; ++i) t += s_sum[i * NL * 8 + c];
+          const int col = u * NL * 8 + c;
+          if (col < d) out[which * d + col] = t;
+        }
+      }
+    }
+}
+
+// dgamma, dbeta: the workgroups' partial rows, 16 at a time side by side, the 16 sums
+// in order.
+constexpr int kRedCols = 64;   // columns per workgroup, four a thread
+__global__ __launch_bounds__(256) void norm_bwd_reduce_kernel(const float* __restrict__ part,
+                                                              int n_part, int d,
+                                                              float* __restrict__ dgamma,
+                                                              float* __restrict__ dbeta) {
+  __shared__ __attribute__((aligned(16))) float s_sum[16][kRedCols];
+  const int lane = threadIdx.x % 16, row = threadIdx.x / 16;
+  const int c = blockIdx.x * kRedCols + lane * 4;   // of the 2 d columns (d % 8 == 0)
+  f32x4_t t = {0.f, 0.f, 0.f, 0.f};
+  if (c < 2 * d) {
+    const float* const p = part + c;
+    for (int i = row; i < n_part; i += 128) {   // eight loads in flight
+      f32x4_t v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        v[u] = i + 16 * u < n_part ? *reinterpret_cast<const f32x4_t*>(p + (size_t)(i + 16 * u) * 2 * d)
+                                   : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < 8; ++u) t += v[u];
+    }
+  }
+  *reinterpret_cast<f32x4_t*>(&s_sum[row][lane * 4]) = t;
+  __syncthreads();
+  const int col = blockIdx.x * kRedCols + threadIdx.x;
+  if (threadIdx.x >= kRedCols || col >= 2 * d) return;
+  float v = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v += s_sum[i][threadIdx.x];
+  if (col < d) dgamma[col] = v;
+  else if (dbeta) dbeta[col - d] = v;
+}
+
+constexpr int kNormThreads = 256, kWideGroups = 1 << 16;
 constexpr int kNormWaves = kNormThreads / kWave;
 
 // Sum over the workgroup, the same bits in every thread (waves in order).
@@ -34,64 +406,67 @@ template <> __device__ __forceinline__ float stored<bf16_t>(float v) {
   return bf16_to_f32(f32_to_bf16(v));
 }
 
-// One workgroup per row.
+// Rows wider than the registers of a workgroup: one workgroup per row, read again
+// for each of its passes.
 template <typename T>
-__global__ __launch_bounds__(kNormThreads) void norm_fwd_kernel(
+__global__ __launch_bounds__(kNormThreads) void norm_fwd_wide_kernel(
     const T* x, const T* residual, const float* __restrict__ gamma,
-    const float* __restrict__ beta, int d, float eps, T* sum_out, T* __restrict__ y,
-    float* __restrict__ mean, float* __restrict__ rstd) {
+    const float* __restrict__ beta, int n_rows, int d, float eps, T* sum_out,
+    T* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd) {
   __shared__ float s_red[kNormWaves];
-  const size_t row = (size_t)blockIdx.x * d;
-  const int nvec = d / 8;
-  auto load = [&](int v, float s[8]) {
-    Elem<T>::load8(x + row + (size_t)v * 8, s);
-    if (residual) {
-      float r[8];
-      Elem<T>::load8(residual + row + (size_t)v * 8, r);
+  for (unsigned r = blockIdx.x; r < (unsigned)n_rows; r += gridDim.x) {
+    const size_t row = (size_t)r * d;
+    const int nvec = d / 8;
+    auto load = [&](int v, float s[8]) {
+      Elem<T>::load8(x + row + (size_t)v * 8, s);
+      if (residual) {
+        float r[8];
+        Elem<T>::load8(residual + row + (size_t)v * 8, r);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) s[q] = stored<T>(s[q] + r[q]);
+        for (int q = 0; q < 8; ++q) s[q] = stored<T>(s[q] + r[q]);
+      }
+    };
+    float sum = 0.0f;
+    for (int v = threadIdx.x; v < nvec; v += kNormThreads) {
+      float s[8];
+      load(v, s);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) sum += s[q];
     }
-  };
-  float sum = 0.0f;
-  for (int v = threadIdx.x; v < nvec; v += kNormThreads) {
-    float s[8];
-    load(v, s);
+    const float mu = block_sum(sum, s_red) / (float)d;
+    float sq = 0.0f;
+    for (int v = threadIdx.x; v < nvec; v += kNormThreads) {
+      float s[8];
+      load(v, s);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) sum += s[q];
-  }
-  const float mu = block_sum(sum, s_red) / (float)d;
-  float sq = 0.0f;
-  for (int v = threadIdx.x; v < nvec; v += kNormThreads) {
-    float s[8];
-    load(v, s);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) sq += (s[q] - mu) * (s[q] - mu);
-  }
-  const float rs = 1.0f / sqrtf(block_sum(sq, s_red) / (float)d + eps);
-  for (int v = threadIdx.x; v < nvec; v += kNormThreads) {
-    float s[8], g[8], o[8];
-    load(v, s);
-    if (sum_out) Elem<T>::store8(sum_out + row + (size_t)v * 8, s);
-    Elem<float>::load8(gamma + (size_t)v * 8, g);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) o[q] = (s[q] - mu) * rs * g[q];
-    if (beta) {
-      Elem<float>::load8(beta + (size_t)v * 8, g);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) o[q] += g[q];
+      for (int q = 0; q < 8; ++q) sq += (s[q] - mu) * (s[q] - mu);
     }
-    Elem<T>::store8(y + row + (size_t)v * 8, o);
-  }
-  if (threadIdx.x == 0) {
-    if (mean) mean[blockIdx.x] = mu;
-    if (rstd) rstd[blockIdx.x] = rs;
+    const float rs = 1.0f / sqrtf(block_sum(sq, s_red) / (float)d + eps);
+    for (int v = threadIdx.x; v < nvec; v += kNormThreads) {
+      float s[8], g[8], o[8];
+      load(v, s);
+      if (sum_out) Elem<T>::store8(sum_out + row + (size_t)v * 8, s);
+      Elem<float>::load8(gamma + (size_t)v * 8, g);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) o[q] = (s[q] - mu) * rs * g[q];
+      if (beta) {
+        Elem<float>::load8(beta + (size_t)v * 8, g);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) o[q] += g[q];
+      }
+      Elem<T>::store8(y + row + (size_t)v * 8, o);
+    }
+    if (threadIdx.x == 0) {
+      if (mean) mean[r] = mu;
+      if (rstd) rstd[r] = rs;
+    }
   }
 }
 
 // One workgroup per range of rows: dx of each, and the range's partial dgamma
-// and dbeta rows, kept in LDS by the thread that owns the columns.
+// and dbeta rows, updated in place by the thread that owns the columns.
 template <typename T>
-__global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(
+__global__ __launch_bounds__(kNormThreads) void norm_bwd_wide_kernel(
     const T* dy, const T* __restrict__ s, const float* __restrict__ gamma,
     const float* __restrict__ mean, const float* __restrict__ rstd, const T* dres, int n_rows,
     int rows_per, int d, T* dx, float* __restrict__ part) {
@@ -147,25 +522,30 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_kernel(
   }
 }
 
-// dgamma, dbeta: the ranges' partial rows in order.
-__global__ __launch_bounds__(256) void norm_bwd_reduce_kernel(const float* __restrict__ part,
-                                                              int n_part, int d,
-                                                              float* __restrict__ dgamma,
-                                                              float* __restrict__ dbeta) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= d) return;
-  float g = 0.0f, b = 0.0f;
-  for (int i = 0; i < n_part; ++i) {
-    g += part[(size_t)i * 2 * d + c];
-    b += part[(size_t)i * 2 * d + d + c];
-  }
-  dgamma[c] = g;
-  if (dbeta) dbeta[c] = b;
+// workgroups of a call: forward, backward (each of these writes its partial sums)
+constexpr int kFwdGroups = 1024, kBwdGroups = 256;
+
+// f(lanes per row, vectors per lane) for rows of nvec vectors: one vector a lane
+// while 512 lanes hold the row, then two or four; false past that.
+template <typename F>
+bool norm_shape(int nvec, F f) {
+  using std::integral_constant;
+  const integral_constant<int, 1> one{};
+  const integral_constant<int, kMaxLanes> most{};
+  if (nvec <= 8) f(integral_constant<int, 8>{}, one);
+  else if (nvec <= 16) f(integral_constant<int, 16>{}, one);
+  else if (nvec <= 32) f(integral_constant<int, 32>{}, one);
+  else if (nvec <= 64) f(integral_constant<int, 64>{}, one);
+  else if (nvec <= 128) f(integral_constant<int, 128>{}, one);
+  else if (nvec <= 256) f(integral_constant<int, 256>{}, one);
+  else if (nvec <= kMaxLanes) f(most, one);
+  else if (nvec <= 2 * kMaxLanes) f(most, integral_constant<int, 2>{});
+  else if (nvec <= 4 * kMaxLanes) f(most, integral_constant<int, 4>{});
+  else return false;
+  return true;
 }
 
-constexpr int kNormParts = 512;
-
-inline int norm_parts(int T) { return T < kNormParts ? T : kNormParts; }
+inline int norm_parts(int T) { return T < kBwdGroups ? T : kBwdGroups; }
 
 }  // namespace
 
@@ -173,14 +553,28 @@ size_t layer_norm_bwd_ws_bytes(int T, int d) {
   return (size_t)norm_parts(T) * 2 * d * sizeof(float);
 }
 
+namespace {
+
 template <typename T>
-static hipError_t norm_fwd_t(const T* x, const T* residual, const float* gamma, const float* beta,
-                             int n, int d, float eps, T* sum_out, T* y, float* mean, float* rstd,
-                             hipStream_t s) {
-  hipLaunchKernelGGL(norm_fwd_kernel<T>, dim3((unsigned)n), dim3(kNormThreads), 0, s, x, residual,
-                     gamma, beta, d, eps, sum_out, y, mean, rstd);
+hipError_t norm_fwd_t(const T* x, const T* residual, const float* gamma, const float* beta, int n,
+                      int d, float eps, T* sum_out, T* y, float* mean, float* rstd,
+                      hipStream_t s) {
+  const bool fits = norm_shape(d / 8, [&](auto nl, auto vpl) {
+    constexpr int NL = decltype(nl)::value, VPL = decltype(vpl)::value;
+    using S = NormShape<NL, kFwdThreads>;
+    const int need = (n - 1) / S::ROWS + 1;
+    hipLaunchKernelGGL((norm_fwd_kernel<T, NL, VPL>),
+                       dim3((unsigned)(need < kFwdGroups ? need : kFwdGroups)), dim3(S::NT), 0, s,
+                       x, residual, gamma, beta, n, d, eps, sum_out, y, mean, rstd);
+  });
+  if (!fits)
+    hipLaunchKernelGGL(norm_fwd_wide_kernel<T>, dim3((unsigned)(n < kWideGroups ? n : kWideGroups)),
+                       dim3(kNormThreads), 0, s, x, residual, gamma, beta, n, d, eps, sum_out, y,
+                       mean, rstd);
   return hipGetLastError();
 }
+
+}  // namespace
 
 hipError_t launch_layer_norm(const void* x, const void* residual, const float* gamma,
                              const float* beta, int dtype, int T, int d, float eps, void* sum_out,
@@ -194,21 +588,34 @@ hipError_t launch_layer_norm(const void* x, const void* residual, const float* g
                     s);
 }
 
+namespace {
+
 template <typename T>
-static hipError_t norm_bwd_t(const T* dy, const T* sv, const float* gamma, const float* mean,
-                             const float* rstd, const T* dres, int n, int d, T* dx, float* dgamma,
-                             float* dbeta, float* part, hipStream_t s) {
-  const int parts = norm_parts(n);
-  const int per = parts ? (n + parts - 1) / parts : 1;
-  const int grid = (n + per - 1) / per;
-  if (grid > 0)
-    hipLaunchKernelGGL(norm_bwd_kernel<T>, dim3((unsigned)grid), dim3(kNormThreads), 0, s, dy, sv,
-                       gamma, mean, rstd, dres, n, per, d, dx, dgamma ? part : nullptr);
+hipError_t norm_bwd_t(const T* dy, const T* sv, const float* gamma, const float* mean,
+                      const float* rstd, const T* dres, int n, int d, T* dx, float* dgamma,
+                      float* dbeta, float* part, hipStream_t s) {
+  int grid = 0;
+  const bool fits = n == 0 || norm_shape(d / 8, [&](auto nl, auto vpl) {
+    constexpr int NL = decltype(nl)::value, VPL = decltype(vpl)::value;
+    using S = NormShape<NL, kBwdThreads>;
+    const int need = (n - 1) / S::ROWS + 1;
+    grid = need < kBwdGroups ? need : kBwdGroups;
+    hipLaunchKernelGGL((norm_bwd_kernel<T, NL, VPL>), dim3((unsigned)grid), dim3(S::NT), 0, s, dy,
+                       sv, gamma, mean, rstd, dres, n, d, dx, dgamma ? part : nullptr);
+  });
+  if (!fits) {
+    const int per = (n - 1) / norm_parts(n) + 1;
+    grid = (n - 1) / per + 1;
+    hipLaunchKernelGGL(norm_bwd_wide_kernel<T>, dim3((unsigned)grid), dim3(kNormThreads), 0, s, dy,
+                       sv, gamma, mean, rstd, dres, n, per, d, dx, dgamma ? part : nullptr);
+  }
   if (dgamma)
-    hipLaunchKernelGGL(norm_bwd_reduce_kernel, dim3((unsigned)((d + 255) / 256)), dim3(256), 0, s,
-                       part, grid, d, dgamma, dbeta);
+    hipLaunchKernelGGL(norm_bwd_reduce_kernel, dim3((unsigned)((2 * d + kRedCols - 1) / kRedCols)),
+                       dim3(256), 0, s, part, grid, d, dgamma, dbeta);
   return hipGetLastError();
 }
+
+}  // namespace
 
 hipError_t launch_layer_norm_bwd(const void* dy, const void* sv, const float* gamma,
                                  const float* mean, const float* rstd, const void* dres, int dtype,
