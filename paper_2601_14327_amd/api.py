@@ -532,7 +532,9 @@ def _want(t: Optional[torch.Tensor], name: str, shape, dtype) -> Optional[torch.
     """A given device tensor of this shape and dtype (None passes)."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype != dtype:
+    if t.shape == shape and t.dtype is dtype and t.is_cuda and t.is_contiguous():
+        return t
+    if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
     return _dev(t, name)
 
@@ -541,6 +543,8 @@ def _out(t: Optional[torch.Tensor], name: str, shape, dtype, device) -> torch.Te
     """The given output buffer, checked, or a new one."""
     if t is None:
         return torch.empty(shape, dtype=dtype, device=device)
+    if t.shape == shape and t.dtype is dtype and t.is_cuda and t.is_contiguous():
+        return t
     return _want(t, name, shape, dtype)
 
 

@@ -6,12 +6,20 @@
 //   loss = coef * mean over the non-empty s of sum_e f[s, e] P[s, e],
 //   c[s, e] = coef f[s, e] / (n_s S_nonempty)     (= dloss / dp[t, e]),
 //   dlogits[t, e] = dloss p_e (c_e - sum_i p_i c_i).
+// HBM-bound where long, launch-bound where short.
+//
 // The tokens are cut into equal chunks, one workgroup each, whatever the sequences:
 // walking chunks and sequences in token order, each step goes to the next chunk or to
 // the next sequence, so the pair (chunk c, sequence s) has the slot c + s to itself,
 // and the partial sums need n_chunks + n_seq slots however the sequences fall.  A
 // second pass sums each sequence's slots in order.  Counts are integers; every
 // floating-point sum has a fixed order.
+//
+// A token's row belongs to G lanes of four experts each (G the power of two from
+// E / 4 up), so a wave reads 64 / G rows at a time in whole lines and a softmax takes
+// log2 G lane moves for its maximum and its sum.
+#include <type_traits>
+
 #include "common.hpp"
 #include "internal.hpp"
 
@@ -21,30 +29,40 @@ namespace {
 constexpr int kBalThreads = 256;
 constexpr int kBalWaves = kBalThreads / kWave;
 constexpr int kBalMaxE = 256;
-constexpr int kBalChunk = 64;      // tokens per workgroup, while that is
-constexpr int kBalMaxChunks = 2048;  // at most so many workgroups
-constexpr int kBalCols = 16;       // experts per workgroup of the second pass
+constexpr int kBalAhead = 4;         // rows of a lane group in flight
+constexpr int kBalIds = 4;           // slots of a thread loaded ahead
+constexpr int kBalMaxChunks = 1024;
+constexpr int kSumThreads = 1024;    // second pass: 16 lanes of four experts, 64 slots side by side
+constexpr int kSumCols = 64, kSumRows = kSumThreads / (kSumCols / 4);
 
 struct BalWs {          // carved from the workspace
   int* live;            // non-empty sequences
-  int* done;            // workgroups of the second pass that have finished
-  float* part_p;        // [slots, E]
-  int* part_n;          // [slots, E]
+  float* part_p;        // [slots, Ep], Ep: E rounded up to 4
+  int* part_n;          // [slots, Ep]
   float* part_loss;     // [n_seq, column blocks]
 };
 
-inline int bal_chunk(int T) {
-  return T <= kBalChunk * kBalMaxChunks ? kBalChunk : (T - 1) / kBalMaxChunks + 1;
+__host__ __device__ inline int bal_ep(int E) { return (E + 3) & ~3; }
+inline int bal_lanes(int E) {
+  int g = 1;
+  while (4 * g < E) g *= 2;
+  return g;
 }
-inline int bal_chunks(int T) { return T > 0 ? (T - 1) / bal_chunk(T) + 1 : 1; }
-// chunks a workspace has to hold: grows with T, so that a workspace for the largest
-// call serves the smaller ones (bal_chunks falls where a chunk gains a token)
-inline int bal_chunks_bound(int T) {
-  const int n = T > 0 ? (T - 1) / kBalChunk + 1 : 1;
-  return n < kBalMaxChunks ? n : kBalMaxChunks;
-}
-inline int bal_blocks(int E) { return (E + kBalCols - 1) / kBalCols; }
+inline int bal_blocks(int E) { return (E + kSumCols - 1) / kSumCols; }
 
+// Tokens per chunk: two passes of the workgroup's rows at least, and 32.
+inline int bal_chunk_least(int E) {
+  const int two = 2 * kBalThreads / bal_lanes(E);
+  return two > 32 ? two : 32;
+}
+inline int bal_chunk(int T, int E) {
+  const int least = bal_chunk_least(E);
+  return T <= least * kBalMaxChunks ? least : (T - 1) / kBalMaxChunks + 1;
+}
+inline int bal_chunks(int T, int E) { return T > 0 ? (T - 1) / bal_chunk(T, E) + 1 : 1; }
+
+// A workspace for the largest call serves the smaller ones: the number of chunks falls
+// where a chunk gains a token or E a lane, so the space is for what never falls.
 inline size_t bal_carve(void* ws, int T, int E, int S, BalWs& w) {
   char* p = static_cast<char*>(ws);
   size_t at = 0;
@@ -53,9 +71,9 @@ inline size_t bal_carve(void* ws, int T, int E, int S, BalWs& w) {
     at += align_up(bytes, 256);
     return r;
   };
-  const size_t cells = ((size_t)bal_chunks_bound(T) + S) * E;
-  w.live = reinterpret_cast<int*>(take(8));
-  w.done = w.live + 1;
+  const int most = T > 0 ? (T - 1) / 32 + 1 : 1;
+  const size_t cells = ((size_t)(most < kBalMaxChunks ? most : kBalMaxChunks) + S) * bal_ep(E);
+  w.live = reinterpret_cast<int*>(take(4));
   w.part_p = reinterpret_cast<float*>(take(cells * 4));
   w.part_n = reinterpret_cast<int*>(take(cells * 4));
   w.part_loss = reinterpret_cast<float*>(take((size_t)S * bal_blocks(E) * 4));
@@ -69,63 +87,114 @@ __device__ __forceinline__ void seq_range(const int32_t* __restrict__ off, int s
   b = off ? min(max(off[s + 1], a), T) : T;
 }
 
-// First sequence that ends after token t (n_seq if none does).
+// First sequence that ends after token t (n_seq if none does), by the whole wave: 64
+// ends are compared at a time, so 64 sequences take one load and not a chain of six.
 __device__ __forceinline__ int first_seq(const int32_t* __restrict__ off, int n_seq, int t) {
   if (!off) return 0;
-  int lo = 0, hi = n_seq;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (off[mid + 1] > t) hi = mid;
-    else lo = mid + 1;
+  const int lane = threadIdx.x & (kWave - 1);
+  int lo = 0, len = n_seq;   // the answer lies in [lo, lo + len]
+  while (len > 0) {
+    const int piece = (len + kWave - 1) / kWave;
+    const bool past = lane * piece < len && off[lo + min((lane + 1) * piece, len)] <= t;
+    const int n = min(__popcll(__ballot(past)) * piece, len);   // ended by t
+    lo += n;
+    len = piece == 1 ? 0 : min(piece - 1, len - n);
   }
   return lo;
 }
 
-// One token's probabilities in a wave: lane l holds experts l, l + 64, ...  A token
-// without an alive expert of finite or infinite logit gets zeros.
-constexpr int kEpl = kBalMaxE / kWave;
-__device__ __forceinline__ void token_probs(const float* __restrict__ row, int E, int lane,
-                                            const bool alive[kEpl], float p[kEpl]) {
+// Four experts of a row, 4 l .. 4 l + 3; VEC: E is a multiple of four.  Streaming loads:
+// what the caches hold is still found there, and the rest does not push out what other
+// calls wrote (131072 x 256, first pass: 43 -> 28 us).
+template <bool VEC>
+__device__ __forceinline__ void load4(const float* __restrict__ row, int e0, int E, float v[4]) {
+  if constexpr (VEC) {
+    const f32x4_t r = ld_stream(reinterpret_cast<const f32x4_t*>(row + e0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = r[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = e0 + i < E ? __builtin_nontemporal_load(row + e0 + i) : 0.0f;
+  }
+}
+
+// Softmax of a row over its G lanes, logits to probabilities.  exp(l - m) is taken as
+// 2^(l log2 e - m log2 e), the rounding of m log2 e being common to the row: one fma
+// and the hardware's exp2 (an ulp) instead of a library call of a dozen instructions.
+// A row without a logit above -inf gets zeros.
+template <int G>
+__device__ __forceinline__ void softmax4(const bool ok[4], float v[4]) {
+  constexpr float kLog2e = 1.44269504f;
   float m = -INFINITY;
 #pragma unroll
-  for (int u = 0; u < kEpl; ++u) {
-    p[u] = alive[u] ? row[lane + kWave * u] : -INFINITY;
-    m = fmaxf(m, p[u]);
+  for (int i = 0; i < 4; ++i) {
+    v[i] = ok[i] ? v[i] : -INFINITY;
+    m = fmaxf(m, v[i]);
   }
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
-  const float base = m == -INFINITY ? 0.0f : m;
+  m = lanes_max<G>(m);
+  const float base = m == -INFINITY ? 0.0f : m * kLog2e;
   float z = 0.0f;
 #pragma unroll
-  for (int u = 0; u < kEpl; ++u) {
-    p[u] = expf(p[u] - base);
-    z += p[u];
+  for (int i = 0; i < 4; ++i) {
+    v[i] = __builtin_amdgcn_exp2f(fmaf(v[i], kLog2e, -base));
+    z += v[i];
   }
-  z = wave_sum(z);
-  const float inv = z == 0.0f ? 0.0f : 1.0f / z;
+  z = lanes_sum<G>(z);
+  const float inv = z == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(z);   // else z >= 1 (or a NaN)
 #pragma unroll
-  for (int u = 0; u < kEpl; ++u) p[u] *= inv;
+  for (int i = 0; i < 4; ++i) v[i] *= inv;
 }
 
-__device__ __forceinline__ void load_alive(const uint8_t* __restrict__ alive, int E, int lane,
-                                           bool a[kEpl]) {
+__device__ __forceinline__ void load_alive(const uint8_t* __restrict__ alive, int E, int e0,
+                                           bool ok[4]) {
+  uint8_t a[4];   // (loaded together, whatever is masked)
 #pragma unroll
-  for (int u = 0; u < kEpl; ++u) {
-    const int e = lane + kWave * u;
-    a[u] = e < E && (alive == nullptr || alive[e] != 0);
-  }
+  for (int i = 0; i < 4; ++i) a[i] = alive == nullptr ? 1 : alive[min(e0 + i, E - 1)];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) ok[i] = e0 + i < E && a[i] != 0;
 }
 
-// First pass: chunk c's probability sums and counts of each sequence in it.
+struct BalOut {
+  float* loss;
+  int32_t* counts;
+  float* prob_mean;
+  float* grad_coef;
+  float coef;
+};
+
+// One expert's outputs of a sequence of len tokens from its sums; returns its share of
+// the loss.
+__device__ __forceinline__ float balance_cell(const BalOut& o, size_t at, float p, int n, int len,
+                                              int k, int n_alive, int live) {
+  float mean = 0.0f, c = 0.0f, part = 0.0f;
+  if (len > 0) {
+    mean = p / (float)len;
+    const float f = (float)n_alive * (float)n / ((float)k * (float)len);
+    part = o.coef * f * mean / (float)live;
+    c = o.coef * f / ((float)len * (float)live);
+  }
+  o.counts[at] = n;
+  o.prob_mean[at] = mean;
+  o.grad_coef[at] = c;
+  return part;
+}
+
+// First pass: chunk c's probability sums and counts of each sequence in it.  ONE: the
+// batch is one chunk, whose workgroup writes the results itself.
+template <int G, bool VEC, bool ONE>
 __global__ __launch_bounds__(kBalThreads) void balance_chunk_kernel(
     const float* __restrict__ logits, const int32_t* __restrict__ topk_idx,
     const uint8_t* __restrict__ alive, const int32_t* __restrict__ off, int T, int E, int k,
-    int n_seq, int chunk, BalWs w) {
-  __shared__ float s_p[kBalWaves][kBalMaxE];
+    int n_seq, int chunk, BalWs w, BalOut o) {
+  constexpr int RPW = kWave / G, ROWS = kBalWaves * RPW;   // rows of a wave, of the workgroup
+  __shared__ __attribute__((aligned(16))) float s_p[kBalWaves][kBalMaxE];
   __shared__ int s_n[kBalMaxE];
   __shared__ int s_live;
+  __shared__ float s_loss[kBalWaves];
   const int tid = threadIdx.x, wave = tid / kWave, lane = tid & (kWave - 1);
-  if (blockIdx.x == 0) {  // what the second pass needs once
+  const int e0 = 4 * (lane % G), ep = bal_ep(E);
+  int n_alive = E;
+  if (ONE || blockIdx.x == gridDim.x - 1) {  // needed once: by the last workgroup, or the one
     if (tid == 0) s_live = 0;
     __syncthreads();
     int n = 0;
@@ -135,161 +204,237 @@ __global__ __launch_bounds__(kBalThreads) void balance_chunk_kernel(
       n += b > a;
     }
     if (n) atomicAdd(&s_live, n);
-    __syncthreads();
-    if (tid == 0) {
-      *w.live = s_live;
-      *w.done = 0;
+    if (ONE && alive) n_alive = __syncthreads_count(tid < E && alive[tid] != 0);
+    else __syncthreads();
+    if (!ONE) {
+      if (tid == 0) *w.live = s_live;
+      return;
     }
   }
-  bool ok[kEpl];
-  load_alive(alive, E, lane, ok);
+  bool ok[4];
+  load_alive(alive, E, e0, ok);
   const int t0 = blockIdx.x * chunk, t1 = T - t0 < chunk ? T : t0 + chunk;
-  for (int s = first_seq(off, n_seq, t0); s < n_seq; ++s) {
+  float loss = 0.0f;
+  for (int s = ONE ? 0 : first_seq(off, n_seq, t0); s < n_seq; ++s) {
     int a, b;
     seq_range(off, s, T, a, b);
-    if (a >= t1) break;
+    if (!ONE && a >= t1) break;
     a = max(a, t0);
     b = min(b, t1);
-    if (a >= b) continue;  // (uniform)
+    if (!ONE && a >= b) continue;  // (uniform)
     for (int e = tid; e < E; e += kBalThreads) s_n[e] = 0;
     __syncthreads();
-    float sum[kEpl] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int t = a + wave; t < b; t += kBalWaves) {
-      float p[kEpl];
-      token_probs(logits + (size_t)t * E, E, lane, ok, p);
+    // the slots' ids: the first ones travel under the logits
+    const size_t i0 = (size_t)a * k + tid, i1 = (size_t)b * k;
+    int ids[kBalIds];
 #pragma unroll
-      for (int u = 0; u < kEpl; ++u) sum[u] += p[u];
+    for (int u = 0; u < kBalIds; ++u)
+      ids[u] = i0 + u * kBalThreads < i1 ? topk_idx[i0 + u * kBalThreads] : -1;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int first = wave * RPW + lane / G;
+    for (int r = 0; r < b - a; r += ROWS * kBalAhead) {  // (uniform: every lane moves along)
+      float v[kBalAhead][4];
+#pragma unroll
+      for (int u = 0; u < kBalAhead; ++u) {
+        const int row = r + u * ROWS + first;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[u][i] = -INFINITY;
+        if (row < b - a && (!VEC || e0 < E))
+          load4<VEC>(logits + (size_t)(a + row) * E, e0, E, v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kBalAhead; ++u) {
+        softmax4<G>(ok, v[u]);   // rows past the sequence: all -inf, zeros
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += v[u][i];
+      }
     }
-    for (size_t i = (size_t)a * k + tid; i < (size_t)b * k; i += kBalThreads) {
+#pragma unroll
+    for (int u = 0; u < kBalIds; ++u)
+      if (ids[u] >= 0 && ids[u] < E) atomicAdd(&s_n[ids[u]], 1);
+    for (size_t i = i0 + kBalIds * kBalThreads; i < i1; i += kBalThreads) {
       const int e = topk_idx[i];
       if (e >= 0 && e < E) atomicAdd(&s_n[e], 1);
     }
 #pragma unroll
-    for (int u = 0; u < kEpl; ++u) s_p[wave][lane + kWave * u] = sum[u];
-    __syncthreads();
-    const size_t slot = ((size_t)blockIdx.x + s) * E;
-    for (int e = tid; e < E; e += kBalThreads) {
-      float v = 0.0f;
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int i = 0; i < kBalWaves; ++i) v += s_p[i][e];
-      w.part_p[slot + e] = v;
-      w.part_n[slot + e] = s_n[e];
+      for (int d = G; d < kWave; d *= 2) sum[i] += __shfl_xor(sum[i], d, kWave);
+    if (lane < G)
+      *reinterpret_cast<f32x4_t*>(&s_p[wave][e0]) = f32x4_t{sum[0], sum[1], sum[2], sum[3]};
+    __syncthreads();
+    if (tid < E) {
+      float p = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kBalWaves; ++i) p += s_p[i][tid];
+      if constexpr (ONE) {
+        loss += balance_cell(o, (size_t)s * E + tid, p, s_n[tid], b - a, k, n_alive, s_live);
+      } else {
+        const size_t at = ((size_t)blockIdx.x + s) * ep + tid;
+        w.part_p[at] = p;
+        w.part_n[at] = s_n[tid];
+      }
     }
     __syncthreads();
   }
+  if constexpr (ONE) {
+    loss = lanes_sum<kWave>(loss);
+    if (lane == 0) s_loss[wave] = loss;
+    __syncthreads();
+    if (tid == 0) {
+      float v = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kBalWaves; ++i) v += s_loss[i];
+      *o.loss = v;
+    }
+  }
 }
 
-// Second pass: 16 experts of one sequence per workgroup, its chunks' sums in order;
-// the workgroup that finishes last adds the loss's parts, in order.
-__global__ __launch_bounds__(kBalThreads) void balance_finish_kernel(
+// Second pass: 64 experts of one sequence per workgroup, its slots 64 side by side and
+// those in order; alone, the workgroup has the loss.
+__global__ __launch_bounds__(kSumThreads) void balance_sum_kernel(
     const uint8_t* __restrict__ alive, const int32_t* __restrict__ off, int T, int E, int k,
-    int n_seq, int chunk, float coef, BalWs w, float* __restrict__ loss, int32_t* __restrict__ counts,
-    float* __restrict__ prob_mean, float* __restrict__ grad_coef) {
-  constexpr int ROWS = kBalThreads / kBalCols;
-  __shared__ float s_p[ROWS][kBalCols];
-  __shared__ int s_n[ROWS][kBalCols];
-  __shared__ float s_l[kBalThreads];
-  __shared__ int s_last;
-  const int tid = threadIdx.x, col = tid % kBalCols, row = tid / kBalCols;
-  const int s = blockIdx.x, e = blockIdx.y * kBalCols + col;
+    int n_seq, int chunk, BalWs w, BalOut o) {
+  __shared__ __attribute__((aligned(16))) float s_p[kSumRows][kSumCols];
+  __shared__ __attribute__((aligned(16))) int s_n[kSumRows][kSumCols];
+  typedef int i32x4_t __attribute__((ext_vector_type(4)));
+  const int tid = threadIdx.x, col = (tid % (kSumCols / 4)) * 4, row = tid / (kSumCols / 4);
+  const int s = blockIdx.x, e = blockIdx.y * kSumCols + col, ep = bal_ep(E);
   const int n_alive = alive == nullptr ? E : __syncthreads_count(tid < E && alive[tid] != 0);
   int a, b;
   seq_range(off, s, T, a, b);
-  float p = 0.0f;
-  int n = 0;
+  f32x4_t p = {0.f, 0.f, 0.f, 0.f};
+  i32x4_t n = {0, 0, 0, 0};
   if (b > a && e < E)
-    for (int c = a / chunk + row; c <= (b - 1) / chunk; c += ROWS) {
-      const size_t at = ((size_t)c + s) * E + e;
-      p += w.part_p[at];
-      n += w.part_n[at];
+    for (int c = a / chunk + row; c <= (b - 1) / chunk; c += kSumRows) {
+      const size_t at = ((size_t)c + s) * ep + e;
+      p += *reinterpret_cast<const f32x4_t*>(w.part_p + at);
+      n += *reinterpret_cast<const i32x4_t*>(w.part_n + at);
     }
-  s_p[row][col] = p;
-  s_n[row][col] = n;
+  *reinterpret_cast<f32x4_t*>(&s_p[row][col]) = p;
+  *reinterpret_cast<i32x4_t*>(&s_n[row][col]) = n;
   __syncthreads();
+  if (tid >= kSumCols) return;   // one wave from here, an expert each
+  const int my = blockIdx.y * kSumCols + tid;
   float part = 0.0f;
-  if (row == 0 && e < E) {
-    p = 0.0f;
-    n = 0;
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-      p += s_p[i][col];
-      n += s_n[i][col];
+  if (my < E) {
+    float ps = 0.0f;
+    int ns = 0;
+#pragma unroll 8
+    for (int i = 0; i < kSumRows; ++i) {
+      ps += s_p[i][tid];
+      ns += s_n[i][tid];
     }
-    const size_t at = (size_t)s * E + e;
-    float mean = 0.0f, c = 0.0f;
-    if (b > a) {
-      const float len = (float)(b - a);
-      mean = p / len;
-      const float f = (float)n_alive * (float)n / ((float)k * len);
-      part = coef * f * mean / (float)*w.live;
-      c = coef * f / (len * (float)*w.live);
-    }
-    counts[at] = n;
-    prob_mean[at] = mean;
-    grad_coef[at] = c;
+    part = balance_cell(o, (size_t)s * E + my, ps, ns, b - a, k, n_alive, *w.live);
   }
-  s_l[tid] = part;
-  __syncthreads();
-  const int n_parts = gridDim.x * gridDim.y;
+  part = lanes_sum<kWave>(part);
   if (tid == 0) {
-    float v = 0.0f;
-    for (int i = 0; i < kBalCols; ++i) v += s_l[i];
-    __hip_atomic_store(&w.part_loss[(size_t)s * gridDim.y + blockIdx.y], v, __ATOMIC_RELAXED,
-                       __HIP_MEMORY_SCOPE_AGENT);
-    s_last = __hip_atomic_fetch_add(w.done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
-             n_parts - 1;
-  }
-  __syncthreads();
-  if (!s_last) return;
-  float v = 0.0f;
-  for (int i = tid; i < n_parts; i += kBalThreads)
-    v += __hip_atomic_load(&w.part_loss[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  s_l[tid] = v;
-  __syncthreads();
-  if (tid < kWave) {
-    v = 0.0f;
-    for (int i = tid; i < kBalThreads; i += kWave) v += s_l[i];
-    v = wave_sum(v);
-    if (tid == 0) *loss = v;
+    if (gridDim.x * gridDim.y == 1) *o.loss = part;
+    else w.part_loss[(size_t)s * gridDim.y + blockIdx.y] = part;
   }
 }
 
-// One wave per token; tokens of no sequence get a zero gradient.
+// The loss's parts, in a fixed order: one wave.
+__global__ __launch_bounds__(kWave) void balance_loss_kernel(const float* __restrict__ part, int n,
+                                                             float* __restrict__ loss) {
+  float v = 0.0f;
+  for (int i = threadIdx.x; i < n; i += 4 * kWave) {
+    float p[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) p[u] = n - i > u * kWave ? part[i + u * kWave] : 0.0f;
+    v += (p[0] + p[1]) + (p[2] + p[3]);
+  }
+  v = lanes_sum<kWave>(v);
+  if (threadIdx.x == 0) *loss = v;
+}
+
+// Backward: a range of tokens per workgroup, walked by sequence with its coefficients
+// in registers; tokens of no sequence get a zero gradient.
+template <int G, bool VEC>
 __global__ __launch_bounds__(kBalThreads) void balance_bwd_kernel(
-    const float* __restrict__ logits, const float* __restrict__ grad_coef,
-    const uint8_t* __restrict__ alive, const int32_t* __restrict__ off,
-    const float* __restrict__ dloss, int T, int E, int n_seq, float* dlogits, int accumulate) {
-  const int lane = threadIdx.x & (kWave - 1);
-  bool ok[kEpl];
-  load_alive(alive, E, lane, ok);
+    const float* logits, const float* __restrict__ grad_coef, const uint8_t* __restrict__ alive,
+    const int32_t* __restrict__ off, const float* __restrict__ dloss, int T, int E, int n_seq,
+    int range, float* dlogits, int accumulate) {
+  constexpr int RPW = kWave / G, ROWS = kBalWaves * RPW;
+  const int tid = threadIdx.x, wave = tid / kWave, lane = tid & (kWave - 1);
+  const int e0 = 4 * (lane % G), first = wave * RPW + lane / G;
+  bool ok[4];
+  load_alive(alive, E, e0, ok);
   const float scale = dloss ? *dloss : 1.0f;
-  const int step = gridDim.x * kBalWaves;
-  for (int t = blockIdx.x * kBalWaves + threadIdx.x / kWave; t < T; t += step) {
-    const int s = first_seq(off, n_seq, t);
-    bool in = s < n_seq;
-    if (in) {
-      int a, b;
-      seq_range(off, s, T, a, b);
-      in = t >= a;
-    }
-    float p[kEpl], c[kEpl];
-    token_probs(logits + (size_t)t * E, E, lane, ok, p);
-    float dot = 0.0f;
+  const int t0 = blockIdx.x * range, t1 = T - t0 < range ? T : t0 + range;
+  auto put = [&](int t, const float v[4]) {
+    float* const d = dlogits + (size_t)t * E + e0;
+    if constexpr (VEC) {
+      if (e0 >= E) return;
+      f32x4_t r = {v[0], v[1], v[2], v[3]};
+      if (accumulate) r += *reinterpret_cast<f32x4_t*>(d);
+      *reinterpret_cast<f32x4_t*>(d) = r;
+    } else {
 #pragma unroll
-    for (int u = 0; u < kEpl; ++u) {
-      c[u] = in && ok[u] ? grad_coef[(size_t)s * E + lane + kWave * u] : 0.0f;
-      dot += p[u] * c[u];
+      for (int i = 0; i < 4; ++i)
+        if (e0 + i < E) d[i] = accumulate ? d[i] + v[i] : v[i];
     }
-    dot = wave_sum(dot);
+  };
+  auto zeros = [&](int from, int to) {
+    const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (!accumulate)
+      for (int t = from + first; t < to; t += ROWS) put(t, z);
+  };
+  int done = t0;
+  for (int s = first_seq(off, n_seq, t0); s < n_seq; ++s) {
+    int a, b;
+    seq_range(off, s, T, a, b);
+    if (a >= t1) break;
+    a = max(a, done);
+    b = min(b, t1);
+    if (a >= b) continue;  // (uniform)
+    zeros(done, a);
+    done = b;
+    float c[4];
 #pragma unroll
-    for (int u = 0; u < kEpl; ++u) {
-      const int e = lane + kWave * u;
-      if (e >= E) continue;
-      float* const o = dlogits + (size_t)t * E + e;
-      const float v = in && ok[u] ? scale * p[u] * (c[u] - dot) : 0.0f;
-      *o = accumulate ? *o + v : v;
+    for (int i = 0; i < 4; ++i) c[i] = ok[i] ? grad_coef[(size_t)s * E + e0 + i] : 0.0f;
+    for (int r = 0; r < b - a; r += ROWS * kBalAhead) {
+      float v[kBalAhead][4];
+#pragma unroll
+      for (int u = 0; u < kBalAhead; ++u) {
+        const int row = r + u * ROWS + first;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[u][i] = -INFINITY;
+        if (row < b - a && (!VEC || e0 < E))
+          load4<VEC>(logits + (size_t)(a + row) * E, e0, E, v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kBalAhead; ++u) {
+        softmax4<G>(ok, v[u]);
+        float dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dot += v[u][i] * c[i];
+        dot = lanes_sum<G>(dot);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[u][i] = ok[i] ? scale * v[u][i] * (c[i] - dot) : 0.0f;
+        const int row = r + u * ROWS + first;
+        if (row < b - a) put(a + row, v[u]);
+      }
     }
-    if (T - t <= step) break;  // (t + step past int32)
+  }
+  zeros(done, t1);
+}
+
+// f(lanes per row, whole vectors) for E experts
+template <typename F>
+void bal_shape(int E, F f) {
+  auto with = [&](auto g) {
+    if (E % 4 == 0) f(g, std::true_type{});
+    else f(g, std::false_type{});
+  };
+  switch (bal_lanes(E)) {
+    case 1: return with(std::integral_constant<int, 1>{});
+    case 2: return with(std::integral_constant<int, 2>{});
+    case 4: return with(std::integral_constant<int, 4>{});
+    case 8: return with(std::integral_constant<int, 8>{});
+    case 16: return with(std::integral_constant<int, 16>{});
+    case 32: return with(std::integral_constant<int, 32>{});
+    default: return with(std::integral_constant<int, 64>{});
   }
 }
 
@@ -306,11 +451,24 @@ hipError_t launch_balance(const float* logits, const int32_t* topk_idx, const ui
                           void* ws, hipStream_t s) {
   BalWs w;
   bal_carve(ws, T, E, n_seq, w);
-  hipLaunchKernelGGL(balance_chunk_kernel, dim3((unsigned)bal_chunks(T)), dim3(kBalThreads), 0, s,
-                     logits, topk_idx, alive, seq_offsets, T, E, k, n_seq, bal_chunk(T), w);
-  hipLaunchKernelGGL(balance_finish_kernel, dim3((unsigned)n_seq, (unsigned)bal_blocks(E)),
-                     dim3(kBalThreads), 0, s, alive, seq_offsets, T, E, k, n_seq, bal_chunk(T), coef, w, loss,
-                     counts, prob_mean, grad_coef);
+  const BalOut o = {loss, counts, prob_mean, grad_coef, coef};
+  const int chunk = bal_chunk(T, E), chunks = bal_chunks(T, E);
+  const bool one = chunks == 1 && n_seq <= 32;
+  const int extra = (T > 0 ? chunks : 0) + 1;   // one workgroup counts the non-empty sequences
+  bal_shape(E, [&](auto g, auto vec) {
+    constexpr int G = decltype(g)::value;
+    constexpr bool VEC = decltype(vec)::value;
+    const auto kernel = one ? balance_chunk_kernel<G, VEC, true> : balance_chunk_kernel<G, VEC, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(one ? 1 : extra)), dim3(kBalThreads), 0, s, logits, topk_idx,
+                       alive, seq_offsets, T, E, k, n_seq, chunk, w, o);
+  });
+  if (one) return hipGetLastError();
+  const int blocks = bal_blocks(E);
+  hipLaunchKernelGGL(balance_sum_kernel, dim3((unsigned)n_seq, (unsigned)blocks),
+                     dim3(kSumThreads), 0, s, alive, seq_offsets, T, E, k, n_seq, chunk, w, o);
+  if (n_seq * blocks > 1)
+    hipLaunchKernelGGL(balance_loss_kernel, dim3(1), dim3(kWave), 0, s, w.part_loss,
+                       n_seq * blocks, loss);
   return hipGetLastError();
 }
 
@@ -318,10 +476,17 @@ hipError_t launch_balance_bwd(const float* logits, const float* grad_coef, const
                               const int32_t* seq_offsets, const float* dloss, int T, int E,
                               int n_seq, float* dlogits, int accumulate, hipStream_t s) {
   if (T == 0) return hipSuccess;
-  const int n = (T - 1) / kBalWaves + 1;
-  hipLaunchKernelGGL(balance_bwd_kernel, dim3((unsigned)(n < 1 << 16 ? n : 1 << 16)),
-                     dim3(kBalThreads), 0, s, logits, grad_coef, alive, seq_offsets, dloss, T, E,
-                     n_seq, dlogits, accumulate);
+  bal_shape(E, [&](auto g, auto vec) {
+    constexpr int G = decltype(g)::value;
+    constexpr int ROWS = kBalThreads / G;
+    // one pass of the rows in flight, longer where the grid would pass 2^14 workgroups
+    const int least = ROWS * kBalAhead, per = (T - 1) / (1 << 14) + 1;
+    const int range = per > least ? per : least;
+    hipLaunchKernelGGL((balance_bwd_kernel<G, decltype(vec)::value>),
+                       dim3((unsigned)((T - 1) / range + 1)), dim3(kBalThreads), 0, s, logits,
+                       grad_coef, alive, seq_offsets, dloss, T, E, n_seq, range, dlogits,
+                       accumulate);
+  });
   return hipGetLastError();
 }
 

@@ -71,7 +71,7 @@ template <> struct Vec8<float> {
 // and 26.  Backward: 256 workgroups of 512 threads, since each writes a row of partial
 // sums, with the next row's loads ahead: 184 us (5.8 TB/s) at 32768 x 4096 with dres,
 // 30 us at 8192 x 2048; 256 threads 186 and 41, 512 workgroups 189 and 34.
-constexpr int kFwdThreads = 256, kBwdThreads = 512, kMaxLanes = 512;
+constexpr int kFwdThreads = 512, kBwdThreads = 512, kMaxLanes = 512;
 template <int NL, int MIN_NT> struct NormShape {
   static constexpr int NT = NL > MIN_NT ? NL : MIN_NT;
   static constexpr int ROWS = NT / NL;                   // rows at a time
@@ -80,10 +80,8 @@ template <int NL, int MIN_NT> struct NormShape {
 
 // sum over the row's lanes inside a wave
 template <int NL>
-__device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-  for (int off = (NL < kWave ? NL : kWave) / 2; off >= 1; off >>= 1) v += __shfl_xor(v, off, kWave);
-  return v;
+__device__ __forceinline__ float row_sum(float v) {
+  return lanes_sum<(NL < kWave ? NL : kWave)>(v);
 }
 
 template <typename T, int NL, int VPL>
@@ -149,7 +147,7 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
     }
     // the wave's own mean and centred squares; several waves' are merged by
     //   M2 = sum_w (M2_w + n_w (mu_w - mu)^2)
-    float mu = cols ? lanes_sum<NL>(sum) / (float)cols : 0.0f;
+    float mu = cols ? row_sum<NL>(sum) / (float)cols : 0.0f;
     float sq = 0.0f;
 #pragma unroll
     for (int u = 0; u < VPL; ++u)
@@ -157,7 +155,7 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
 #pragma unroll
         for (int q = 0; q < 8; ++q) sq += (s[u][q] - mu) * (s[u][q] - mu);
       }
-    sq = lanes_sum<NL>(sq);
+    sq = row_sum<NL>(sq);
     if constexpr (S::WAVES > 1) {
       if (threadIdx.x % kWave == 0) {
         s_red[it][wave][0] = mu;
@@ -284,8 +282,8 @@ __global__ __launch_bounds__((NormShape<NL, kBwdThreads>::NT)) void norm_bwd_ker
       }
     }
     if (AHEAD && more) load(row + step);
-    a = lanes_sum<NL>(a);
-    b = lanes_sum<NL>(b);
+    a = row_sum<NL>(a);
+    b = row_sum<NL>(b);
     if constexpr (S::WAVES > 1) {
       if (threadIdx.x % kWave == 0) {
         s_red[it][wave][0] = a;
@@ -523,7 +521,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_wide_kernel(
 }
 
 // workgroups of a call: forward, backward (each of these writes its partial sums)
-constexpr int kFwdGroups = 1024, kBwdGroups = 256;
+constexpr int kFwdGroups = 512, kBwdGroups = 256;
 
 // f(lanes per row, vectors per lane) for rows of nvec vectors: one vector a lane
 // while 512 lanes hold the row, then two or four; false past that.
