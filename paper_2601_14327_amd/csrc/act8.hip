@@ -14,6 +14,11 @@
 namespace laep {
 namespace {
 
+// HBM-bound; one vector of 8 columns a thread and no loop while the grid allows: 16
+// columns a thread took 178 us and persistent grids of 1024 to 4096 workgroups 146 to
+// 160 us against 132 (6.1 TB/s) for save and load of 65536 x 2048 bf16.  Stores stream:
+// what they write is read much later, or by a product that reads it many times
+// (ordinary ones: 141 us, and 122 against 111 in the SwiGLU backward at d_ff 1024).
 constexpr int kActThreads = 256;
 constexpr uint32_t kActNan = 255;
 
@@ -63,7 +68,7 @@ __global__ __launch_bounds__(kActThreads) void act8_save_kernel(const T* __restr
   for (long long i = (long long)blockIdx.x * kActThreads + threadIdx.x; i < n_vec;
        i += (long long)gridDim.x * kActThreads) {
     float v[8];
-    Elem<T>::load8_stream(act + i * 8, v);
+    Elem<T>::load8(act + i * 8, v);
     uint32_t m = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -78,7 +83,7 @@ __global__ __launch_bounds__(kActThreads) void act8_save_kernel(const T* __restr
       w[0] = act8_quant4(v, inv);
       w[1] = act8_quant4(v + 4, inv);
     }
-    q[i] = w;
+    __builtin_nontemporal_store(w, q + i);
     if ((threadIdx.x & 3) == 0) scale[i >> 2] = (uint8_t)b;
   }
 }
@@ -92,15 +97,16 @@ __global__ __launch_bounds__(kActThreads) void act8_load_kernel(const u32x2_t* _
        i += (long long)gridDim.x * kActThreads) {
     float v[8];
     act8_decode8(q[i], act8_scale(scale[i >> 2]), v);
-    Elem<T>::store8(act + i * 8, v);
+    Elem<T>::store8_stream(act + i * 8, v);
   }
 }
 
 // SwiGLU backward, one vector of 8 columns of one row per thread: with A_g and
 // A_u decoded and s = sigmoid(A_g),
 //   dA_g = dH A_u s (1 + A_g (1 - s)),  dA_u = dH silu(A_g),  H = silu(A_g) A_u.
-// h may be dh (each thread reads its vector before it writes it).
-template <typename T>
+// h may be dh (each thread reads its vector before it writes it).  STREAM: dh's loads
+// stream, see the launch.
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(kActThreads) void swiglu_bwd_act8_kernel(
     const u32x2_t* __restrict__ q, const uint8_t* __restrict__ scale, const T* dh, long long R,
     int f, T* __restrict__ da, T* h) {
@@ -113,7 +119,8 @@ __global__ __launch_bounds__(kActThreads) void swiglu_bwd_act8_kernel(
     float ag[8], au[8], d[8], og[8], ou[8], oh[8];
     act8_decode8(q[g], act8_scale(scale[g >> 2]), ag);
     act8_decode8(q[u], act8_scale(scale[u >> 2]), au);
-    Elem<T>::load8(dh + i * 8, d);
+    if constexpr (STREAM) Elem<T>::load8_stream(dh + i * 8, d);
+    else Elem<T>::load8(dh + i * 8, d);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float sg = fast_sigmoid(ag[e]);
@@ -122,9 +129,9 @@ __global__ __launch_bounds__(kActThreads) void swiglu_bwd_act8_kernel(
       ou[e] = d[e] * sl;
       oh[e] = sl * au[e];
     }
-    Elem<T>::store8(da + g * 8, og);
-    Elem<T>::store8(da + u * 8, ou);
-    Elem<T>::store8(h + i * 8, oh);
+    Elem<T>::store8_stream(da + g * 8, og);
+    Elem<T>::store8_stream(da + u * 8, ou);
+    Elem<T>::store8_stream(h + i * 8, oh);
   }
 }
 
@@ -162,18 +169,35 @@ hipError_t launch_act8_load(const void* q, const uint8_t* scale, int dtype, int6
   return hipGetLastError();
 }
 
+namespace {
+
+template <typename T, bool STREAM>
+void swiglu_bwd_act8_t(const void* q, const uint8_t* scale, const void* dh, int64_t R, int f,
+                       void* da, void* h, hipStream_t s) {
+  hipLaunchKernelGGL((swiglu_bwd_act8_kernel<T, STREAM>), act_grid(R * (long long)(f / 8)),
+                     dim3(kActThreads), 0, s, static_cast<const u32x2_t*>(q), scale,
+                     static_cast<const T*>(dh), (long long)R, f, static_cast<T*>(da),
+                     static_cast<T*>(h));
+}
+
+}  // namespace
+
 hipError_t launch_swiglu_bwd_act8(const void* q, const uint8_t* scale, const void* dh, int dtype,
                                   int64_t R, int f, void* da, void* h, hipStream_t s) {
-  const long long n = R * (long long)(f / 8);
-  if (n == 0) return hipSuccess;
-  if (dtype == kDtypeBf16)
-    hipLaunchKernelGGL(swiglu_bwd_act8_kernel<bf16_t>, act_grid(n), dim3(kActThreads), 0, s,
-                       static_cast<const u32x2_t*>(q), scale, static_cast<const bf16_t*>(dh),
-                       (long long)R, f, static_cast<bf16_t*>(da), static_cast<bf16_t*>(h));
-  else
-    hipLaunchKernelGGL(swiglu_bwd_act8_kernel<float>, act_grid(n), dim3(kActThreads), 0, s,
-                       static_cast<const u32x2_t*>(q), scale, static_cast<const float*>(dh),
-                       (long long)R, f, static_cast<float*>(da), static_cast<float*>(h));
+  if (R == 0) return hipSuccess;
+  // dh, which the product before has just written, streams once the call's bytes pass
+  // what the 256 MB last-level cache holds: 65536 rows of d_ff 1024 (675 MB) 117 us with
+  // ordinary loads, 103 streaming; 12000 of 2048 (248 MB) 42.5 / 38.6; 3062 of 2048
+  // (63 MB) 10.6 / 12.4.
+  const int64_t elem = dtype == kDtypeBf16 ? 2 : 4;
+  const bool stream = R * f * (2 + 4 * elem) > (int64_t)224 << 20;
+  if (dtype == kDtypeBf16) {
+    if (stream) swiglu_bwd_act8_t<bf16_t, true>(q, scale, dh, R, f, da, h, s);
+    else swiglu_bwd_act8_t<bf16_t, false>(q, scale, dh, R, f, da, h, s);
+  } else {
+    if (stream) swiglu_bwd_act8_t<float, true>(q, scale, dh, R, f, da, h, s);
+    else swiglu_bwd_act8_t<float, false>(q, scale, dh, R, f, da, h, s);
+  }
   return hipGetLastError();
 }
 
