@@ -50,19 +50,26 @@ inline int bal_lanes(int E) {
 }
 inline int bal_blocks(int E) { return (E + kSumCols - 1) / kSumCols; }
 
-// Tokens per chunk: two passes of the workgroup's rows at least, and 32.
-inline int bal_chunk_least(int E) {
-  const int two = 2 * kBalThreads / bal_lanes(E);
-  return two > 32 ? two : 32;
+// Tokens per chunk: two passes of the workgroup's rows at least, and 32; fewer where that
+// would put many sequences into a chunk, which takes them one after the other (about
+// 0.7 us each: 60 sequences of 500 tokens in all over 2 experts 45 us in one chunk).
+constexpr int kBalLeast = 8;
+inline int bal_cut(int tokens, int T, int n_seq) {   // to about two sequences
+  const int two = 2 * (T / n_seq);
+  if (n_seq == 1 || two >= tokens) return tokens;
+  return two > kBalLeast ? two : kBalLeast;
 }
-inline int bal_chunk(int T, int E) {
-  const int least = bal_chunk_least(E);
-  return T <= least * kBalMaxChunks ? least : (T - 1) / kBalMaxChunks + 1;
+inline int bal_chunk(int T, int E, int n_seq) {
+  const int rows = 2 * kBalThreads / bal_lanes(E);
+  const int least = bal_cut(rows > 32 ? rows : 32, T, n_seq);
+  const int few = T > 0 ? (T - 1) / kBalMaxChunks + 1 : 1;
+  return few > least ? few : least;
 }
-inline int bal_chunks(int T, int E) { return T > 0 ? (T - 1) / bal_chunk(T, E) + 1 : 1; }
+inline int bal_chunks(int T, int chunk) { return T > 0 ? (T - 1) / chunk + 1 : 1; }
 
 // A workspace for the largest call serves the smaller ones: the number of chunks falls
-// where a chunk gains a token or E a lane, so the space is for what never falls.
+// where a chunk gains a token, E a lane or n_seq a sequence, so the space is for what
+// never falls.
 inline size_t bal_carve(void* ws, int T, int E, int S, BalWs& w) {
   char* p = static_cast<char*>(ws);
   size_t at = 0;
@@ -71,7 +78,7 @@ inline size_t bal_carve(void* ws, int T, int E, int S, BalWs& w) {
     at += align_up(bytes, 256);
     return r;
   };
-  const int most = T > 0 ? (T - 1) / 32 + 1 : 1;
+  const int most = T > 0 ? (T - 1) / kBalLeast + 1 : 1;
   const size_t cells = ((size_t)(most < kBalMaxChunks ? most : kBalMaxChunks) + S) * bal_ep(E);
   w.live = reinterpret_cast<int*>(take(4));
   w.part_p = reinterpret_cast<float*>(take(cells * 4));
@@ -452,8 +459,8 @@ hipError_t launch_balance(const float* logits, const int32_t* topk_idx, const ui
   BalWs w;
   bal_carve(ws, T, E, n_seq, w);
   const BalOut o = {loss, counts, prob_mean, grad_coef, coef};
-  const int chunk = bal_chunk(T, E), chunks = bal_chunks(T, E);
-  const bool one = chunks == 1 && n_seq <= 32;
+  const int chunk = bal_chunk(T, E, n_seq), chunks = bal_chunks(T, chunk);
+  const bool one = chunks == 1 && n_seq <= 4;
   const int extra = (T > 0 ? chunks : 0) + 1;   // one workgroup counts the non-empty sequences
   bal_shape(E, [&](auto g, auto vec) {
     constexpr int G = decltype(g)::value;
@@ -479,8 +486,9 @@ hipError_t launch_balance_bwd(const float* logits, const float* grad_coef, const
   bal_shape(E, [&](auto g, auto vec) {
     constexpr int G = decltype(g)::value;
     constexpr int ROWS = kBalThreads / G;
-    // one pass of the rows in flight, longer where the grid would pass 2^14 workgroups
-    const int least = ROWS * kBalAhead, per = (T - 1) / (1 << 14) + 1;
+    // one pass of the rows in flight, about two sequences at most; longer where the grid
+    // would pass 2^14 workgroups
+    const int least = bal_cut(ROWS * kBalAhead, T, n_seq), per = (T - 1) / (1 << 14) + 1;
     const int range = per > least ? per : least;
     hipLaunchKernelGGL((balance_bwd_kernel<G, decltype(vec)::value>),
                        dim3((unsigned)((T - 1) / range + 1)), dim3(kBalThreads), 0, s, logits,
