@@ -108,6 +108,31 @@ int moe_balance_loss_bwd(const float* logits, const float* grad_coef,
                          const float* dloss, int T, int E, int n_seq,
                          float* dlogits, int accumulate, void* stream);
 
+/*
+ * moe_route_bwd_balance -- moe_route_bwd of a router trained with a balance
+ * loss: the loss's gradient is added to the gates' before the products.
+ *
+ *   dl[t, e] = moe_route_bwd's dl[t, e]
+ *              + dloss * p_e (c_e - sum_i p_i c_i),  c = grad_coef[s, :]
+ *   dlogits, dw_router, dbias, dx from that dl, as moe_route_bwd forms them.
+ *   Every alive expert carries a gradient, so the products are dense for
+ *   renormalised gates too, and offsets and row_src are not needed.
+ *
+ *   logits device [T, E] float32 (moe_route's output, both kinds of gates);
+ *   grad_coef, seq_offsets, n_seq, dloss as in moe_balance_loss_bwd; the other
+ *   arguments, the workspace and T = 0 as in moe_route_bwd.
+ */
+int moe_route_bwd_balance(const float* dgate, const int32_t* topk_idx,
+                          const float* topk_gate, const float* logits,
+                          const uint8_t* alive, const void* x,
+                          const void* w_router, const float* grad_coef,
+                          const int32_t* seq_offsets, int n_seq,
+                          const float* dloss, int dtype, int T, int d_model,
+                          int E, int k, int renorm, float* dlogits,
+                          float* dw_router, float* dbias, void* dx,
+                          int accumulate_dx, void* ws, size_t ws_bytes,
+                          void* stream);
+
 /* Columns that share one scale of an 8-bit activation checkpoint. */
 #define LAEP_ACT8_BLOCK 32
 
@@ -147,6 +172,25 @@ int moe_act8_load(const int8_t* q, const uint8_t* scale, int dtype, int64_t R,
 int moe_swiglu_bwd_act8(const int8_t* q, const uint8_t* scale, const void* dh,
                         int dtype, int64_t R, int d_ff, void* da, void* h,
                         void* stream);
+
+/*
+ * moe_grouped_ffn_bwd_gather_act8 -- moe_grouped_ffn_bwd_gather at
+ * pre-activations kept in 8 bits (moe_act8_save of act_save): the SwiGLU
+ * backward decodes them, and dW_d takes the H recomputed there, so neither
+ * act_save nor the forward's H is needed.  Results are bit-identical to
+ * moe_grouped_ffn_bwd_gather with act_save = moe_act8_load(q, scale) and
+ * h_fwd NULL.
+ *
+ *   act_q device [R, 2*d_ff] int8, act_scale device [R, 2*d_ff / 32] uint8;
+ *   the other arguments and the workspace as in moe_grouped_ffn_bwd_gather.
+ */
+int moe_grouped_ffn_bwd_gather_act8(
+    const void* dy_perm, const void* dout, const float* topk_gate,
+    const void* x, const int32_t* row_src, int T, int k, const int8_t* act_q,
+    const uint8_t* act_scale, const void* w_gate_up, const void* w_down,
+    const int32_t* offsets, const int32_t* expert_map, int dtype, int E,
+    int d_model, int d_ff, int64_t R, void* dx_perm, float* dw_gate_up,
+    float* dw_down, int accumulate, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

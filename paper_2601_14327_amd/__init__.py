@@ -24,8 +24,11 @@ and what a pre-norm MoE block computes around them:
     moe_layer_norm, moe_layer_norm_bwd      residual add and layer norm, gradients
     moe_balance_loss, moe_balance_loss_bwd  balance loss per batch or sequence, expert
                          counts, the logits' gradient
+    moe_route_bwd_balance                   the router's backward with that gradient
     moe_act8_save, moe_act8_load            activations kept in 8 bits
-    moe_swiglu_bwd_act8  the SwiGLU backward at them
+    moe_swiglu_bwd_act8, moe_grouped_ffn_bwd_gather_act8
+                         the SwiGLU and the whole expert backward at them
+    MoEBlockPlan         all of it as one training step of a pre-norm block
 
     laep_calib_copy, laep_calib_read,  measurement calls (attained peaks,
     laep_calib_mfma                    the router's feed bound)
@@ -55,6 +58,7 @@ from .api import (  # noqa: F401
     moe_expert_counts,
     moe_grouped_ffn_bwd,
     moe_grouped_ffn_bwd_gather,
+    moe_grouped_ffn_bwd_gather_act8,
     moe_grouped_ffn_fwd,
     moe_grouped_ffn_fwd_gather,
     moe_grouped_ffn_fwd_gather_combine,
@@ -64,11 +68,13 @@ from .api import (  # noqa: F401
     moe_permute_bwd,
     moe_route,
     moe_route_bwd,
+    moe_route_bwd_balance,
     moe_route_count,
     moe_route_count_noalloc,
     moe_swiglu_bwd_act8,
     workspace_bytes,
 )
+from .block import BlockWeights, MoEBlockPlan  # noqa: F401
 from .layer import MoELayerPlan, layer_forward  # noqa: F401
 from .placement import placement_report  # noqa: F401
 from .pruning import ExpertPruner, compact_layer, hybrid_alpha  # noqa: F401

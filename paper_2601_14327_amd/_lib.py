@@ -86,6 +86,10 @@ SIGNATURES = {
     "moe_layer_norm_bwd": (_i, [_p, _p, _p, _p, _p, _p, _i, _i, _i, _p, _p, _p, _p, _sz, _p]),
     "moe_balance_loss": (_i, [_p, _p, _p, _p, _i, _i, _i, _i, _f, _p, _p, _p, _p, _p, _sz, _p]),
     "moe_balance_loss_bwd": (_i, [_p, _p, _p, _p, _p, _i, _i, _i, _p, _i, _p]),
+    "moe_route_bwd_balance": (_i, [_p, _p, _p, _p, _p, _p, _p, _p, _p, _i, _p, _i, _i, _i, _i, _i,
+                                   _i, _p, _p, _p, _p, _i, _p, _sz, _p]),
+    "moe_grouped_ffn_bwd_gather_act8": (_i, [_p, _p, _p, _p, _p, _i, _i, _p, _p, _p, _p, _p, _p,
+                                             _i, _i, _i, _i, _i64, _p, _p, _p, _i, _p, _sz, _p]),
     "moe_act8_save": (_i, [_p, _i, _i64, _i, _p, _p, _p]),
     "moe_act8_load": (_i, [_p, _p, _i, _i64, _i, _p, _p]),
     "moe_swiglu_bwd_act8": (_i, [_p, _p, _p, _i, _i64, _i, _p, _p, _p]),

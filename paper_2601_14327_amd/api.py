@@ -142,7 +142,7 @@ def moe_expert_counts(topk_idx: torch.Tensor, E: int, *, want_row_src: bool = Fa
 def moe_route_count(x: torch.Tensor, w_router: torch.Tensor, k: int, *, bias=None, alive=None,
                     renorm: bool = True, want_logits: bool = False, want_row_src: bool = False,
                     etn_accum=None, ws=None, topk_idx=None, topk_gate=None, counts=None,
-                    offsets=None, dest_row=None, row_src=None):
+                    offsets=None, dest_row=None, row_src=None, logits=None):
     """Routing and expert counts in one call.  Returns (topk_idx, topk_gate,
     counts, offsets, dest_row, row_src or None, logits or None)."""
     _dev(x, "x"), _dev(w_router, "w_router")
@@ -158,7 +158,8 @@ def moe_route_count(x: torch.Tensor, w_router: torch.Tensor, k: int, *, bias=Non
     dest_row = torch.empty(T * k, dtype=i32, device=dev) if dest_row is None else dest_row
     if want_row_src and row_src is None:
         row_src = torch.empty(T * k, dtype=i32, device=dev)
-    logits = torch.empty((T, E), dtype=torch.float32, device=dev) if want_logits else None
+    if want_logits and logits is None:
+        logits = torch.empty((T, E), dtype=torch.float32, device=dev)
     ws = _workspace(ws, workspace_bytes(LAEP_CALL_COUNTS, T, k, E), dev)
     check(lib().moe_route_count(_ptr(x), _ptr(w_router), _ptr(bias), _ptr(alive), _dtype_code(x),
                                 T, d, E, k, int(renorm), _ptr(logits), _ptr(topk_idx),
@@ -591,11 +592,13 @@ def moe_layer_norm_bwd(dy: torch.Tensor, s: torch.Tensor, gamma: torch.Tensor,
     dx = _out(dx, "dx", (T, d), s.dtype, dev)
     dgamma = _out(dgamma, "dgamma", (d,), f32, dev) if weights else None
     dbeta = _out(dbeta, "dbeta", (d,), f32, dev) if weights and want_dbeta else None
-    ws = _workspace(ws, workspace_bytes(LAEP_CALL_LAYER_NORM_BWD, T, 1, 1, d) if weights else 0,
-                    dev)
+    if weights:
+        ws = _given_ws(ws, dev, LAEP_CALL_LAYER_NORM_BWD, T, 1, 1, d)
     check(lib().moe_layer_norm_bwd(_ptr(dy), _ptr(s), _ptr(gamma), _ptr(mean), _ptr(rstd),
                                    _ptr(dres), code, T, d, _ptr(dx), _ptr(dgamma), _ptr(dbeta),
-                                   _ptr(ws), ws.numel() * ws.element_size(), _stream(dev)))
+                                   _ptr(ws) if weights else None,
+                                   ws.numel() * ws.element_size() if weights else 0,
+                                   _stream(dev)))
     return dx, dgamma, dbeta
 
 
@@ -606,6 +609,19 @@ def _sequences(seq_offsets) -> int:
         raise ValueError("seq_offsets must be an int32 tensor [n_seq + 1]")
     _dev(seq_offsets, "seq_offsets")
     return seq_offsets.numel() - 1
+
+
+def _given_ws(ws, device, which, *sizes):
+    """The given workspace (its size is the C call's to check) or a new one."""
+    if ws is None:
+        return torch.empty(max(workspace_bytes(which, *sizes), 1), dtype=torch.uint8,
+                           device=device)
+    return ws
+
+
+def _scalar(t, name: str):
+    if t is not None and (t.dtype is not torch.float32 or t.numel() != 1 or not t.is_cuda):
+        raise ValueError(f"{name} must be a float32 device tensor of one element")
 
 
 def moe_balance_loss(logits: torch.Tensor, topk_idx: torch.Tensor, *, coef: float = 1.0,
@@ -628,7 +644,7 @@ def moe_balance_loss(logits: torch.Tensor, topk_idx: torch.Tensor, *, coef: floa
     counts = _out(counts, "counts", (S, E), torch.int32, dev)
     prob_mean = _out(prob_mean, "prob_mean", (S, E), f32, dev)
     grad_coef = _out(grad_coef, "grad_coef", (S, E), f32, dev)
-    ws = _workspace(ws, workspace_bytes(LAEP_CALL_BALANCE, T, S, E), dev)
+    ws = _given_ws(ws, dev, LAEP_CALL_BALANCE, T, S, E)
     check(lib().moe_balance_loss(_ptr(logits), _ptr(topk_idx), _ptr(alive), _ptr(seq_offsets), T,
                                  E, k, S, float(coef), _ptr(loss), _ptr(counts), _ptr(prob_mean),
                                  _ptr(grad_coef), _ptr(ws), ws.numel() * ws.element_size(),
@@ -647,8 +663,7 @@ def moe_balance_loss_bwd(logits: torch.Tensor, grad_coef: torch.Tensor, *, dloss
     f32 = torch.float32
     _want(logits, "logits", (T, E), f32), _want(grad_coef, "grad_coef", (S, E), f32)
     _want(alive, "alive", (E,), torch.uint8)
-    if dloss is not None and (dloss.dtype != f32 or dloss.numel() != 1 or not dloss.is_cuda):
-        raise ValueError("dloss must be a float32 device tensor of one element")
+    _scalar(dloss, "dloss")
     if accumulate and dlogits is None:
         raise ValueError("accumulate needs dlogits")
     dlogits = _out(dlogits, "dlogits", (T, E), f32, logits.device)
@@ -656,6 +671,48 @@ def moe_balance_loss_bwd(logits: torch.Tensor, grad_coef: torch.Tensor, *, dloss
                                      _ptr(seq_offsets), _ptr(dloss), T, E, S, _ptr(dlogits),
                                      int(accumulate), _stream(logits.device)))
     return dlogits
+
+
+def moe_route_bwd_balance(dgate: torch.Tensor, topk_idx: torch.Tensor, topk_gate: torch.Tensor,
+                          logits: torch.Tensor, x: torch.Tensor, w_router: torch.Tensor,
+                          grad_coef: torch.Tensor, *, seq_offsets=None, dloss=None,
+                          renorm: bool = True, alive=None, dx=None, accumulate_dx: bool = False,
+                          want_dlogits: bool = False, want_dbias: bool = False, dw_router=None,
+                          dlogits=None, dbias=None, ws=None, data: bool = True,
+                          weights: bool = True):
+    """moe_route_bwd with the balance loss's gradient (moe_balance_loss's
+    grad_coef) added to the gates' before the products.  Returns as moe_route_bwd."""
+    for t, n in ((dgate, "dgate"), (topk_idx, "topk_idx"), (topk_gate, "topk_gate"), (x, "x"),
+                 (w_router, "w_router")):
+        _dev(t, n)
+    T, k = topk_idx.shape
+    E, d = w_router.shape
+    dev = x.device
+    f32 = torch.float32
+    S = _sequences(seq_offsets)
+    _want(logits, "logits", (T, E), f32), _want(grad_coef, "grad_coef", (S, E), f32)
+    _want(alive, "alive", (E,), torch.uint8)
+    _scalar(dloss, "dloss")
+    if data:
+        if dx is None:   # overwritten whole unless accumulated onto
+            dx = torch.zeros_like(x) if accumulate_dx else torch.empty_like(x)
+    else:
+        dx = None
+    if weights:
+        dw_router = _out(dw_router, "dw_router", (E, d), f32, dev)
+        if want_dbias:
+            dbias = _out(dbias, "dbias", (E,), f32, dev)
+    else:
+        dw_router, dbias = None, None
+    if want_dlogits or dlogits is not None:
+        dlogits = _out(dlogits, "dlogits", (T, E), f32, dev)
+    ws = _workspace(ws, workspace_bytes(LAEP_CALL_ROUTE_BWD, T, k, E, d), dev)
+    check(lib().moe_route_bwd_balance(
+        _ptr(dgate), _ptr(topk_idx), _ptr(topk_gate), _ptr(logits), _ptr(alive), _ptr(x),
+        _ptr(w_router), _ptr(grad_coef), _ptr(seq_offsets), S, _ptr(dloss), _dtype_code(x), T, d,
+        E, k, int(renorm), _ptr(dlogits), _ptr(dw_router), _ptr(dbias), _ptr(dx),
+        int(accumulate_dx), _ptr(ws), ws.numel() * ws.element_size(), _stream(dev)))
+    return dx, dw_router, dbias, dlogits
 
 
 def moe_act8_save(act: torch.Tensor, *, q=None, scale=None):
@@ -700,6 +757,45 @@ def moe_swiglu_bwd_act8(q: torch.Tensor, scale: torch.Tensor, dh: torch.Tensor, 
     check(lib().moe_swiglu_bwd_act8(_ptr(q), _ptr(scale), _ptr(dh), _dtype_code(dh), R, f,
                                     _ptr(da), _ptr(h), _stream(dh.device)))
     return da, h
+
+
+def moe_grouped_ffn_bwd_gather_act8(dy_perm, x, row_src, k: int, act_q, act_scale, w_gate_up,
+                                    w_down, offsets, *, dout=None, topk_gate=None,
+                                    expert_map=None, dw_gate_up=None, dw_down=None,
+                                    accumulate=False, ws=None, dx_perm=None,
+                                    return_ws: bool = False):
+    """moe_grouped_ffn_bwd_gather at pre-activations kept in 8 bits (act_q [R, 2f],
+    act_scale [R, 2f/32]); dW_d takes the H recomputed there.  Returns as
+    moe_grouped_ffn_bwd."""
+    for t, n in ((x, "x"), (row_src, "row_src"), (w_gate_up, "w_gate_up"), (w_down, "w_down"),
+                 (offsets, "offsets")):
+        _dev(t, n)
+    if dy_perm is None:
+        if dout is None or topk_gate is None:
+            raise ValueError("without dy_perm, dout and topk_gate are needed")
+        _dev(dout, "dout"), _dev(topk_gate, "topk_gate")
+    else:
+        _dev(dy_perm, "dy_perm")
+    T, d = x.shape
+    R = row_src.shape[0]
+    f = w_down.shape[2]
+    E = offsets.shape[0] - 1
+    dev = x.device
+    _want(act_q, "act_q", (R, 2 * f), torch.int8)
+    _want(act_scale, "act_scale", (R, 2 * f // LAEP_ACT8_BLOCK), torch.uint8)
+    dx_perm = torch.empty((R, d), dtype=x.dtype, device=dev) if dx_perm is None else dx_perm
+    if dw_gate_up is None:
+        dw_gate_up = torch.empty(w_gate_up.shape, dtype=torch.float32, device=dev)
+    if dw_down is None:
+        dw_down = torch.empty(w_down.shape, dtype=torch.float32, device=dev)
+    ws = _workspace(ws, workspace_bytes(LAEP_CALL_FFN_BWD, R, 1, E, d, f), dev)
+    check(lib().moe_grouped_ffn_bwd_gather_act8(
+        _ptr(dy_perm), _ptr(dout), _ptr(topk_gate), _ptr(x), _ptr(row_src), T, k, _ptr(act_q),
+        _ptr(act_scale), _ptr(w_gate_up), _ptr(w_down), _ptr(offsets), _ptr(expert_map),
+        _dtype_code(x), E, d, f, R, _ptr(dx_perm), _ptr(dw_gate_up), _ptr(dw_down),
+        int(accumulate), _ptr(ws), ws.numel(), _stream(dev)))
+    out = (dx_perm, dw_gate_up, dw_down)
+    return out + (ws,) if return_ws else out
 
 
 # ---- measurement calls (laep_calib.h) -------------------------------------------------

@@ -368,6 +368,60 @@ int moe_route_bwd(const float* dgate, const int32_t* topk_idx, const float* topk
                     "moe_route_bwd");
 }
 
+}  // extern "C"
+
+namespace {
+
+// sequences of the balance loss: offsets, or none for one sequence of all tokens
+int check_sequences(const char* name, const int32_t* seq_offsets, int n_seq) {
+  REQUIRE(n_seq >= 1 && n_seq <= LAEP_MAX_SEQUENCES, LAEP_ERR_INVALID_ARG,
+          "%s: n_seq=%d outside [1, %d]", name, n_seq, LAEP_MAX_SEQUENCES);
+  REQUIRE(seq_offsets || n_seq == 1, LAEP_ERR_INVALID_ARG,
+          "%s: n_seq=%d needs seq_offsets (without them the batch is one sequence)", name, n_seq);
+  return LAEP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int moe_route_bwd_balance(const float* dgate, const int32_t* topk_idx, const float* topk_gate,
+                          const float* logits, const uint8_t* alive, const void* x,
+                          const void* w_router, const float* grad_coef,
+                          const int32_t* seq_offsets, int n_seq, const float* dloss, int dtype,
+                          int T, int d_model, int E, int k, int renorm, float* dlogits,
+                          float* dw_router, float* dbias, void* dx, int accumulate_dx, void* ws,
+                          size_t ws_bytes, void* stream) {
+  int rc = check_dtype(dtype);
+  if (rc) return rc;
+  if ((rc = check_experts(E, k))) return rc;
+  if ((rc = check_rows(T, k, d_model))) return rc;
+  if ((rc = check_sequences("moe_route_bwd_balance", seq_offsets, n_seq))) return rc;
+  REQUIRE(w_router, LAEP_ERR_INVALID_ARG, "moe_route_bwd_balance: w_router must be non-null");
+  REQUIRE(dw_router || !dbias, LAEP_ERR_INVALID_ARG,
+          "moe_route_bwd_balance: dbias needs dw_router (they are computed together)");
+  REQUIRE(aligned16(w_router) && aligned16(dw_router), LAEP_ERR_INVALID_ARG,
+          "moe_route_bwd_balance: w_router and dw_router must be 16-byte aligned");
+  if (T > 0) {
+    REQUIRE(dgate && topk_idx && topk_gate && logits && grad_coef && x && ws, LAEP_ERR_INVALID_ARG,
+            "moe_route_bwd_balance: dgate, topk_idx, topk_gate, logits, grad_coef, x and ws must "
+            "be non-null");
+    REQUIRE(aligned16(x) && aligned16(dx) && aligned16(logits) && aligned16(dlogits) &&
+                aligned16(ws),
+            LAEP_ERR_INVALID_ARG,
+            "moe_route_bwd_balance: x, dx, logits, dlogits and ws must be 16-byte aligned");
+    const size_t need = laep::route_bwd_ws_bytes(T, k, E, d_model);
+    REQUIRE(ws_bytes >= need, LAEP_ERR_WORKSPACE,
+            "moe_route_bwd_balance: workspace %zu < %zu bytes", ws_bytes, need);
+  }
+  const laep::BalanceGrad balance = {grad_coef, seq_offsets, dloss, n_seq};
+  return hip_status(laep::launch_route_bwd(dgate, topk_idx, topk_gate, logits, alive, x, w_router,
+                                           nullptr, nullptr, dtype, T, d_model, E, k, renorm,
+                                           dlogits, dw_router, dbias, dx, accumulate_dx, ws,
+                                           as_stream(stream), &balance),
+                    "moe_route_bwd_balance");
+}
+
 int moe_permute(const void* x, int dtype, const int32_t* dest_row, int T, int k, int d_model,
                 void* x_perm, void* stream) {
   int rc = check_dtype(dtype);
@@ -552,6 +606,46 @@ int moe_grouped_ffn_bwd_gather(const void* dy_perm, const void* dout, const floa
                     "moe_grouped_ffn_bwd_gather");
 }
 
+int moe_grouped_ffn_bwd_gather_act8(const void* dy_perm, const void* dout, const float* topk_gate,
+                                    const void* x, const int32_t* row_src, int T, int k,
+                                    const int8_t* act_q, const uint8_t* act_scale,
+                                    const void* w_gate_up, const void* w_down,
+                                    const int32_t* offsets, const int32_t* expert_map, int dtype,
+                                    int E, int d_model, int d_ff, int64_t R, void* dx_perm,
+                                    float* dw_gate_up, float* dw_down, int accumulate, void* ws,
+                                    size_t ws_bytes, void* stream) {
+  int rc = check_ffn_shape(dtype, E, d_model, d_ff, R);
+  if (rc) return rc;
+  REQUIRE(dtype == LAEP_BF16, LAEP_ERR_UNSUPPORTED,
+          "moe_grouped_ffn_bwd_gather_act8: only LAEP_BF16 is supported");
+  REQUIRE(T >= 0 && k >= 1, LAEP_ERR_INVALID_ARG, "moe_grouped_ffn_bwd_gather_act8: T=%d, k=%d", T, k);
+  REQUIRE(R <= (int64_t)T * k, LAEP_ERR_INVALID_ARG,
+          "moe_grouped_ffn_bwd_gather_act8: R=%lld exceeds T*k", (long long)R);
+  REQUIRE((int64_t)T * d_model * 2 < kMaxBufferBytes, LAEP_ERR_UNSUPPORTED,
+          "moe_grouped_ffn_bwd_gather_act8: x (T*d_model bf16) must be under 2 GiB");
+  REQUIRE(offsets && dw_gate_up && dw_down && ws, LAEP_ERR_INVALID_ARG,
+          "moe_grouped_ffn_bwd_gather_act8: offsets, dw_gate_up, dw_down and ws must be non-null");
+  REQUIRE(R == 0 || (x && row_src && act_q && act_scale && w_gate_up && w_down && dx_perm),
+          LAEP_ERR_INVALID_ARG,
+          "moe_grouped_ffn_bwd_gather_act8: activation pointers and row_src must be non-null");
+  REQUIRE(R == 0 || dy_perm || (dout && topk_gate), LAEP_ERR_INVALID_ARG,
+          "moe_grouped_ffn_bwd_gather_act8: without dy_perm, dout and topk_gate must be non-null");
+  REQUIRE(aligned16(dy_perm) && aligned16(dout) && aligned16(x) && aligned16(act_q) &&
+              aligned16(act_scale) &&
+              aligned16(w_gate_up) && aligned16(w_down) && aligned16(dx_perm) &&
+              aligned16(dw_gate_up) && aligned16(dw_down) && aligned16(ws),
+          LAEP_ERR_INVALID_ARG, "moe_grouped_ffn_bwd_gather_act8: buffers must be 16-byte aligned");
+  const size_t need = laep::ffn_bwd_ws_bytes(R, E, d_model, d_ff, dtype);
+  REQUIRE(ws_bytes >= need, LAEP_ERR_WORKSPACE,
+          "moe_grouped_ffn_bwd_gather_act8: workspace %zu < %zu bytes", ws_bytes, need);
+  return hip_status(laep::launch_ffn_bwd_bf16(dy_perm, x, act_q, nullptr, w_gate_up, w_down,
+                                              offsets, expert_map, E, d_model, d_ff, R, dx_perm,
+                                              dw_gate_up, dw_down, accumulate != 0, ws,
+                                              as_stream(stream), row_src, k, T, dout, topk_gate,
+                                              act_scale),
+                    "moe_grouped_ffn_bwd_gather_act8");
+}
+
 int moe_combine(const void* y_perm, const float* topk_gate, const int32_t* dest_row, int T, int k,
                 int d_model, int dtype, void* out, void* stream) {
   int rc = check_dtype(dtype);
@@ -654,23 +748,6 @@ int moe_layer_norm_bwd(const void* dy, const void* s, const float* gamma, const 
                                                 dx, dgamma, dbeta, ws, as_stream(stream)),
                     "moe_layer_norm_bwd");
 }
-
-}  // extern "C"
-
-namespace {
-
-// sequences of the balance loss: offsets, or none for one sequence of all tokens
-int check_sequences(const char* name, const int32_t* seq_offsets, int n_seq) {
-  REQUIRE(n_seq >= 1 && n_seq <= LAEP_MAX_SEQUENCES, LAEP_ERR_INVALID_ARG,
-          "%s: n_seq=%d outside [1, %d]", name, n_seq, LAEP_MAX_SEQUENCES);
-  REQUIRE(seq_offsets || n_seq == 1, LAEP_ERR_INVALID_ARG,
-          "%s: n_seq=%d needs seq_offsets (without them the batch is one sequence)", name, n_seq);
-  return LAEP_OK;
-}
-
-}  // namespace
-
-extern "C" {
 
 int moe_balance_loss(const float* logits, const int32_t* topk_idx, const uint8_t* alive,
                      const int32_t* seq_offsets, int T, int E, int k, int n_seq, float coef,

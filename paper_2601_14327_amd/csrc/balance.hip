@@ -22,6 +22,7 @@
 
 #include "common.hpp"
 #include "internal.hpp"
+#include "lanes.hpp"
 
 namespace laep {
 namespace {

@@ -769,7 +769,7 @@ hipError_t launch_ffn_bwd_bf16(const void* dy, const void* x_perm, const void* a
                                int f, int64_t R, void* dx_perm, float* dw_gu, float* dw_d,
                                int accumulate, void* ws, hipStream_t s, const int32_t* row_src,
                                int slots_k, int64_t x_rows, const void* dout,
-                               const float* gate) {
+                               const float* gate, const uint8_t* act_scale) {
   // dy == NULL: data gradient 1 and dW_d form dY on load from dout and the gates
   const bool dy_on_load = dy == nullptr;
   char* base = static_cast<char*>(ws);
@@ -865,7 +865,9 @@ hipError_t launch_ffn_bwd_bf16(const void* dy, const void* x_perm, const void* a
   if (err == hipSuccess)
     err = dy_on_load ? launch_bwd<EPI_STORE, false, false, true>(g, max_ragged * g.n_tiles_n, s)
                      : launch_bwd<EPI_STORE, false>(g, max_ragged * g.n_tiles_n, s);
-  if (err == hipSuccess && R > 0) {
+  if (err == hipSuccess && act_scale) {
+    err = launch_swiglu_bwd_act8(act_save, act_scale, Hb, kDtypeBf16, R, f, dA, Hb, s);
+  } else if (err == hipSuccess && R > 0) {
     const long long n_vec = R * (long long)(f / 8);
     hipLaunchKernelGGL(swiglu_bwd_kernel, dim3((unsigned)((n_vec + 255) / 256)), dim3(256), 0, s,
                        static_cast<const u32x4_t*>(act_save), (int64_t)R, f,

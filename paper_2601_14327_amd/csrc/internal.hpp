@@ -110,6 +110,8 @@ size_t ffn_bwd_hb_offset(int64_t R, int f, int dtype);
 // else H_b, recomputed at the saved pre-activations.
 // row_src != NULL: x_perm is the token rows x [x_rows, d] and the weight
 // gradient reads routed row r from token row row_src[r] / slots_k.
+// act_scale != NULL: act_save is the 8-bit checkpoint q [R, 2f] with these scales
+// (h_fwd must then be NULL).
 // dy == NULL (with row_src): dY is formed on load from dout [x_rows, d] and the
 // flat gates [x_rows * slots_k], as round(gate[s] * dout[s / slots_k]).
 hipError_t launch_ffn_bwd_bf16(const void* dy, const void* x_perm, const void* act_save,
@@ -119,16 +121,23 @@ hipError_t launch_ffn_bwd_bf16(const void* dy, const void* x_perm, const void* a
                                void* dx_perm, float* dw_gu, float* dw_d, int accumulate,
                                void* ws, hipStream_t s, const int32_t* row_src = nullptr,
                                int slots_k = 1, int64_t x_rows = 0, const void* dout = nullptr,
-                               const float* gate = nullptr);
+                               const float* gate = nullptr, const uint8_t* act_scale = nullptr);
 
-// Router backward.
+// Router backward; with `balance` (and the logits) the balance loss's gradient of the
+// logits is added to the gates'.
+struct BalanceGrad {
+  const float* grad_coef;       // [n_seq, E]
+  const int32_t* seq_offsets;   // [n_seq + 1] or NULL
+  const float* dloss;           // [1] or NULL
+  int n_seq;
+};
 size_t route_bwd_ws_bytes(int T, int k, int E, int d_model);
 hipError_t launch_route_bwd(const float* dgate, const int32_t* idx, const float* gate,
                             const float* logits, const uint8_t* alive, const void* x,
                             const void* w_router, const int32_t* offsets, const int32_t* row_src,
                             int dtype, int T, int d, int E, int k, int renorm, float* dlogits,
                             float* dw_router, float* dbias, void* dx, int accumulate_dx, void* ws,
-                            hipStream_t s);
+                            hipStream_t s, const BalanceGrad* balance = nullptr);
 
 // Layer norm of the block's rows, and its backward (ws: the partial weight gradients).
 hipError_t launch_layer_norm(const void* x, const void* residual, const float* gamma,

@@ -9,6 +9,7 @@
 
 #include "common.hpp"
 #include "internal.hpp"
+#include "lanes.hpp"
 
 namespace laep {
 namespace {

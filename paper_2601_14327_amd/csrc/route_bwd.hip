@@ -691,16 +691,34 @@ hipError_t launch_route_bwd_t(const float* dgate, const int32_t* idx, const floa
                               const T* w_router, const int32_t* offsets, const int32_t* row_src,
                               int T_, int d, int E, int k, int renorm, float* dlogits,
                               float* dw_router, float* dbias, T* dx, int accumulate_dx, void* ws,
-                              hipStream_t s) {
+                              hipStream_t s, const BalanceGrad* balance) {
   float* dl = static_cast<float*>(ws);  // [T, k]
   float* dl_dense = reinterpret_cast<float*>(static_cast<char*>(ws) +
                                              align_up((size_t)T_ * k * sizeof(float), 256));
   char* base = reinterpret_cast<char*>(dl_dense) + align_up((size_t)T_ * E * sizeof(float), 256);
-  if (!renorm) {
-    const int lanes = E <= 32 ? dl_lanes(E) : 64;
-    const auto dl_full = lanes < 64 ? route_bwd_dl_full_kernel<true> : route_bwd_dl_full_kernel<false>;
-    hipLaunchKernelGGL(dl_full, dl_grid(T_, 64 / lanes), dim3(kDlThreads), 0, s, dgate, idx, gate,
-                       logits, alive, T_, E, k, lanes, dl_dense, dlogits);
+  // with a balance loss every alive expert carries a gradient, whatever the gates: the
+  // gates' dl is written dense (into dlogits when that is wanted), the loss's added, and
+  // the dense products follow as for full-softmax gates
+  if (balance && dlogits) {
+    dl_dense = dlogits;
+    dlogits = nullptr;
+  }
+  if (!renorm || balance) {
+    if (renorm) {
+      hipLaunchKernelGGL(route_bwd_dl_kernel, dl_grid(T_, 1), dim3(kDlThreads), 0, s, dgate, idx,
+                         gate, T_, E, k, dl, dl_dense, static_cast<float*>(nullptr));
+    } else {
+      const int lanes = E <= 32 ? dl_lanes(E) : 64;
+      const auto dl_full = lanes < 64 ? route_bwd_dl_full_kernel<true> : route_bwd_dl_full_kernel<false>;
+      hipLaunchKernelGGL(dl_full, dl_grid(T_, 64 / lanes), dim3(kDlThreads), 0, s, dgate, idx, gate,
+                         logits, alive, T_, E, k, lanes, dl_dense, dlogits);
+    }
+    if (balance) {
+      const hipError_t err =
+          launch_balance_bwd(logits, balance->grad_coef, alive, balance->seq_offsets,
+                             balance->dloss, T_, E, balance->n_seq, dl_dense, 1, s);
+      if (err != hipSuccess) return err;
+    }
     if (dx && dx_by_rows(T_, E))
       hipLaunchKernelGGL(route_bwd_dx_kernel<T>, dim3((unsigned)((T_ + 3) / 4)), dim3(256), 0, s,
                          w_router, static_cast<const int32_t*>(nullptr), dl_dense, T_, E, d,
@@ -752,7 +770,7 @@ hipError_t launch_route_bwd(const float* dgate, const int32_t* idx, const float*
                             const void* w_router, const int32_t* offsets, const int32_t* row_src,
                             int dtype, int T_, int d, int E, int k, int renorm, float* dlogits,
                             float* dw_router, float* dbias, void* dx, int accumulate_dx, void* ws,
-                            hipStream_t s) {
+                            hipStream_t s, const BalanceGrad* balance) {
   if (T_ == 0) {
     // no tokens: zero weight gradients (dx has no rows)
     if (dw_router)
@@ -764,11 +782,11 @@ hipError_t launch_route_bwd(const float* dgate, const int32_t* idx, const float*
     return launch_route_bwd_t(dgate, idx, gate, logits, alive, static_cast<const bf16_t*>(x),
                               static_cast<const bf16_t*>(w_router), offsets, row_src, T_, d, E, k,
                               renorm, dlogits, dw_router, dbias, static_cast<bf16_t*>(dx),
-                              accumulate_dx, ws, s);
+                              accumulate_dx, ws, s, balance);
   return launch_route_bwd_t(dgate, idx, gate, logits, alive, static_cast<const float*>(x),
                             static_cast<const float*>(w_router), offsets, row_src, T_, d, E, k,
                             renorm, dlogits, dw_router, dbias, static_cast<float*>(dx),
-                            accumulate_dx, ws, s);
+                            accumulate_dx, ws, s, balance);
 }
 
 }  // namespace laep

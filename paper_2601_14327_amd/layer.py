@@ -23,6 +23,11 @@ Backward:
 In a training step the router's weight gradients need only the gate gradient:
 backward(router=...) runs them on a side stream beside the expert backward and
 takes the router's dx after moe_permute_bwd.
+With act_bits=8 the pre-activations that a training step keeps are stored in 8
+bits (moe_act8_save) and the backward reads those
+(moe_grouped_ffn_bwd_gather_act8): 2.06 d_ff bytes a routed row are kept instead
+of the 6 d_ff of act_save and H, which become scratch that plans run one after
+the other can share (``scratch``).
 
 All buffers are allocated once, so a pass makes no allocation and no host
 synchronisation; every step runs in the library's kernels on the current
@@ -36,13 +41,19 @@ from typing import Optional
 import torch
 
 from . import api
-from ._lib import LAEP_CALL_COUNTS, LAEP_CALL_FFN_BWD, LAEP_CALL_FFN_FWD, LAEP_CALL_ROUTE_BWD
+from ._lib import (LAEP_ACT8_BLOCK, LAEP_CALL_COUNTS, LAEP_CALL_FFN_BWD, LAEP_CALL_FFN_FWD,
+                   LAEP_CALL_ROUTE_BWD)
 
 
 class MoELayerPlan:
     def __init__(self, T: int, d_model: int, E: int, k: int, d_ff: int,
                  dtype: torch.dtype = torch.bfloat16, device="cuda", backward: bool = False,
-                 save_act: Optional[bool] = None, fused_dispatch: Optional[bool] = None):
+                 save_act: Optional[bool] = None, fused_dispatch: Optional[bool] = None,
+                 act_bits: int = 16, scratch: Optional["MoELayerPlan"] = None):
+        """``act_bits`` 8: a training plan (bf16, fused dispatch) keeps its
+        pre-activations in 8 bits.  ``scratch``: a plan of the same sizes and kind
+        whose transient buffers this one uses too; their forward and backward
+        passes must not overlap."""
         self.T, self.d, self.E, self.k, self.f = T, d_model, E, k, d_ff
         self.R = T * k
         self.dtype = dtype
@@ -65,6 +76,15 @@ class MoELayerPlan:
         if fused_dispatch is None:
             fused_dispatch = dtype == torch.bfloat16
         self.fused = bool(fused_dispatch)
+        if act_bits not in (8, 16):
+            raise ValueError(f"act_bits={act_bits} is neither 8 nor 16")
+        if act_bits == 8 and not (backward and save_act and self.fused):
+            raise ValueError("act_bits=8 needs a training plan with the fused dispatch (bf16)")
+        self.act_bits = act_bits
+        kind = (T, d_model, E, k, d_ff, dtype, dev, backward, self.fused, act_bits)
+        if scratch is not None and scratch.kind != kind:
+            raise ValueError("scratch must be a plan of the same sizes and kind")
+        self.kind = kind
         self.x_perm = (None if self.fused and (backward or not save_act) else
                        torch.empty((R, d_model), dtype=dtype, device=dev))
         self.x_in = None   # the token rows of the last forward (the gathered backward reads them)
@@ -78,38 +98,56 @@ class MoELayerPlan:
         self.fused_combine = k == 1 and self.fused
         self.y_perm = (None if self.fused_combine and not (backward or save_act) else
                        torch.empty((R, d_model), dtype=dtype, device=dev))
-        self.act_save = (torch.empty((R, 2 * d_ff), dtype=dtype, device=dev) if save_act
-                         else None)
+        if scratch is not None and act_bits == 8:   # transient: decoded into 8 bits at once
+            self.act_save = scratch.act_save
+        else:
+            self.act_save = (torch.empty((R, 2 * d_ff), dtype=dtype, device=dev) if save_act
+                             else None)
+        if act_bits == 8:
+            self.act_q = torch.empty((R, 2 * d_ff), dtype=torch.int8, device=dev)
+            self.act_scale = torch.empty((R, 2 * d_ff // LAEP_ACT8_BLOCK), dtype=torch.uint8,
+                                         device=dev)
         self.out = torch.empty((T, d_model), dtype=dtype, device=dev)
-        self.ws_counts = torch.empty(max(1, api.workspace_bytes(LAEP_CALL_COUNTS, T, k, E)),
-                                     dtype=torch.uint8, device=dev)
-        self.ws_ffn = torch.empty(api.workspace_bytes(LAEP_CALL_FFN_FWD, R, 1, E, d_model, d_ff),
-                                  dtype=torch.uint8, device=dev)
+        if scratch is not None:
+            self.ws_counts = scratch.ws_counts
+        else:
+            self.ws_counts = torch.empty(max(1, api.workspace_bytes(LAEP_CALL_COUNTS, T, k, E)),
+                                         dtype=torch.uint8, device=dev)
+        # (a 16-bit training plan's H stays in ws_ffn for its backward)
+        if scratch is not None and (act_bits == 8 or not backward):
+            self.ws_ffn = scratch.ws_ffn
+        else:
+            self.ws_ffn = torch.empty(
+                api.workspace_bytes(LAEP_CALL_FFN_FWD, R, 1, E, d_model, d_ff),
+                dtype=torch.uint8, device=dev)
         if backward:
-            self.dy_perm = (None if self.fused else
-                            torch.empty((R, d_model), dtype=dtype, device=dev))
             # dY of a fused plan: written by the combine backward, read by the data
             # gradient and dW_d of the same call (formed on load by both instead,
             # each column block scaling its rows again, the training step of 8192
             # tokens, top-8, d 2048, d_ff 1024 takes 3.12 ms against 3.03, that of
             # 32768 rows, d 4096, d_ff 2048 5.29 against 5.06)
-            self._dy = (torch.empty((R, d_model), dtype=dtype, device=dev) if self.fused
-                        else self.dy_perm)
-            self.dx_perm = torch.empty((R, d_model), dtype=dtype, device=dev)
+            if scratch is not None:
+                self._dy, self.dx_perm, self.ws_bwd = scratch._dy, scratch.dx_perm, scratch.ws_bwd
+                self.ws_route_bwd = scratch.ws_route_bwd
+                self.ws_route_bwd_w = scratch.ws_route_bwd_w
+            else:
+                self._dy = torch.empty((R, d_model), dtype=dtype, device=dev)
+                self.dx_perm = torch.empty((R, d_model), dtype=dtype, device=dev)
+                self.ws_bwd = torch.empty(
+                    api.workspace_bytes(LAEP_CALL_FFN_BWD, R, 1, E, d_model, d_ff),
+                    dtype=torch.uint8, device=dev)
+                rb = max(1, api.workspace_bytes(LAEP_CALL_ROUTE_BWD, T, k, E, d_model))
+                self.ws_route_bwd = torch.empty(rb, dtype=torch.uint8, device=dev)
+                # the router's weight gradients run on a side stream beside the expert
+                # backward, with a workspace of their own
+                self.ws_route_bwd_w = torch.empty(rb, dtype=torch.uint8, device=dev)
+            self.dy_perm = None if self.fused else self._dy
             self.dgate = torch.empty((T, k), dtype=torch.float32, device=dev)
             self.dx = torch.empty((T, d_model), dtype=dtype, device=dev)
-            self.ws_bwd = torch.empty(
-                api.workspace_bytes(LAEP_CALL_FFN_BWD, R, 1, E, d_model, d_ff),
-                dtype=torch.uint8, device=dev)
             self.dw_gate_up = None
             self.dw_down = None
             self.dw_router = None
             self.dbias = None
-            rb = max(1, api.workspace_bytes(LAEP_CALL_ROUTE_BWD, T, k, E, d_model))
-            self.ws_route_bwd = torch.empty(rb, dtype=torch.uint8, device=dev)
-            # the router's weight gradients run on a side stream beside the expert
-            # backward, with a workspace of their own
-            self.ws_route_bwd_w = torch.empty(rb, dtype=torch.uint8, device=dev)
             self._side = None
             self._side_done = None
 
@@ -143,6 +181,7 @@ class MoELayerPlan:
                 keep_y=self.y_perm is not None, y_perm=self.y_perm,
                 save_act=self.act_save is not None, act_save=self.act_save,
                 x_perm_out=self.x_perm)
+            self._keep_act()
             return self.out
         if self.fused:
             # x_perm (kept for inspection only) by the token-major permute, which
@@ -159,8 +198,13 @@ class MoELayerPlan:
             api.moe_grouped_ffn_fwd(self.x_perm, w_gate_up, w_down, self.offsets,
                                     expert_map=expert_map, ws=self.ws_ffn, y_perm=self.y_perm,
                                     save_act=self.act_save is not None, act_save=self.act_save)
+        self._keep_act()
         api.moe_combine(self.y_perm, self.topk_gate, self.dest_row, out=self.out)
         return self.out
+
+    def _keep_act(self):
+        if self.act_bits == 8:
+            api.moe_act8_save(self.act_save, q=self.act_q, scale=self.act_scale)
 
     # -- whole passes ----------------------------------------------------------
     def forward(self, x, w_router, w_gate_up, w_down, bias=None, renorm=True,
@@ -192,7 +236,18 @@ class MoELayerPlan:
                           dbias=self.dbias if want_dbias else None, ws=self.ws_route_bwd)
         return self.dx, self.dw_router
 
-    def route_backward_weights_async(self, x, w_router, want_dbias=False):
+    def _route_bwd(self, x, w_router, balance, **kw):
+        """moe_route_bwd, or with ``balance`` (moe_route_bwd_balance's logits,
+        grad_coef and options) that call."""
+        if balance is None:
+            api.moe_route_bwd(self.dgate, self.topk_idx, self.topk_gate, x, w_router, renorm=True,
+                              offsets=self.offsets, row_src=self.row_src, **kw)
+        else:
+            b = dict(balance)
+            api.moe_route_bwd_balance(self.dgate, self.topk_idx, self.topk_gate, b.pop("logits"),
+                                      x, w_router, b.pop("grad_coef"), **b, **kw)
+
+    def route_backward_weights_async(self, x, w_router, want_dbias=False, balance=None):
         """dw_router (and dbias) from self.dgate on a side stream, started now:
         they need only the gate gradient, so they can run beside the expert
         backward.  route_backward_data waits for them."""
@@ -205,37 +260,46 @@ class MoELayerPlan:
         main = torch.cuda.current_stream(self.device)
         self._side.wait_stream(main)
         with torch.cuda.stream(self._side):
-            api.moe_route_bwd(self.dgate, self.topk_idx, self.topk_gate, x, w_router,
-                              renorm=True, offsets=self.offsets, row_src=self.row_src,
-                              data=False, dw_router=self.dw_router,
-                              want_dbias=want_dbias, dbias=self.dbias if want_dbias else None,
-                              ws=self.ws_route_bwd_w)
+            self._route_bwd(x, w_router, balance, data=False, dw_router=self.dw_router,
+                            want_dbias=want_dbias, dbias=self.dbias if want_dbias else None,
+                            ws=self.ws_route_bwd_w)
             self._side_done.record(self._side)
 
-    def route_backward_data(self, x, w_router):
+    def route_backward_data(self, x, w_router, balance=None):
         """The router's dx, accumulated onto self.dx; then the current stream
         waits for route_backward_weights_async."""
-        api.moe_route_bwd(self.dgate, self.topk_idx, self.topk_gate, x, w_router, renorm=True,
-                          offsets=self.offsets, row_src=self.row_src, dx=self.dx,
-                          accumulate_dx=True, weights=False, ws=self.ws_route_bwd)
+        self._route_bwd(x, w_router, balance, dx=self.dx, accumulate_dx=True, weights=False,
+                        ws=self.ws_route_bwd)
         torch.cuda.current_stream(self.device).wait_event(self._side_done)
         return self.dx, self.dw_router
 
     def backward(self, dout, w_gate_up, w_down, expert_map=None, accumulate=False,
-                 router=None, want_dbias=False):
+                 router=None, want_dbias=False, balance=None):
         """Expert backward; with router=(x, w_router) (renormalised gates) also
-        the router's, its weight gradients beside the expert backward."""
+        the router's, its weight gradients beside the expert backward.
+        ``balance``: the router was trained with a balance loss; a dict of
+        moe_route_bwd_balance's logits, grad_coef and options (either gates)."""
         api.moe_combine_bwd(dout, self.y_perm, self.topk_gate, self.dest_row,
                             dy_perm=self._dy, dgate=self.dgate)
         if router is not None:
-            self.route_backward_weights_async(router[0], router[1], want_dbias=want_dbias)
+            self.route_backward_weights_async(router[0], router[1], want_dbias=want_dbias,
+                                              balance=balance)
         if self.dw_gate_up is None:
             self.dw_gate_up = torch.empty(w_gate_up.shape, dtype=torch.float32,
                                           device=self.device)
             self.dw_down = torch.empty(w_down.shape, dtype=torch.float32, device=self.device)
-        # dW_d from the H the forward computed (left in its workspace)
-        h_fwd = api.ffn_fwd_h_view(self.ws_ffn, self.R, self.f, self.dtype)
-        if self.fused:   # X gathered from the forward's token rows
+        # dW_d from the H the forward computed (left in its workspace); at 8-bit
+        # pre-activations from the H recomputed there
+        h_fwd = (None if self.act_bits == 8 else
+                 api.ffn_fwd_h_view(self.ws_ffn, self.R, self.f, self.dtype))
+        if self.act_bits == 8:
+            api.moe_grouped_ffn_bwd_gather_act8(self._dy, self.x_in, self.row_src, self.k,
+                                                self.act_q, self.act_scale, w_gate_up, w_down,
+                                                self.offsets, expert_map=expert_map,
+                                                dw_gate_up=self.dw_gate_up, dw_down=self.dw_down,
+                                                accumulate=accumulate, ws=self.ws_bwd,
+                                                dx_perm=self.dx_perm)
+        elif self.fused:   # X gathered from the forward's token rows
             api.moe_grouped_ffn_bwd_gather(self._dy, self.x_in, self.row_src, self.k,
                                            self.act_save, w_gate_up, w_down, self.offsets,
                                            h_fwd=h_fwd, expert_map=expert_map,
@@ -249,7 +313,7 @@ class MoELayerPlan:
                                     accumulate=accumulate, ws=self.ws_bwd, dx_perm=self.dx_perm)
         api.moe_permute_bwd(self.dx_perm, self.dest_row, self.T, self.k, out=self.dx)
         if router is not None:
-            self.route_backward_data(router[0], router[1])
+            self.route_backward_data(router[0], router[1], balance=balance)
         return self.dx, self.dgate, self.dw_gate_up, self.dw_down
 
 

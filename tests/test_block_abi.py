@@ -175,3 +175,47 @@ def test_binding_refuses_on_the_device():
         laep.moe_act8_load(z(4, 64, dt=torch.int8), z(4, 2, dt=torch.uint8), torch.float16)
     with pytest.raises(ValueError, match="q must"):
         laep.moe_swiglu_bwd_act8(z(4, 64, dt=torch.int8), z(4, 2, dt=torch.uint8), x)
+
+
+def test_router_backward_with_balance_refusals(L):
+    keep, p = _fake()
+    need = L.moe_workspace_bytes(4, 16, 2, 8, 64, 0)
+
+    def call(**kw):
+        a = dict(dict(dg=p, i=p, g=p, l=p, al=None, x=p, w=p, gc=p, off=None, S=1, dl=None, dt=1,
+                      T=16, d=64, E=8, k=2, out=None, dw=p, db=None, dx=p, ws=p, n=need), **kw)
+        return L.moe_route_bwd_balance(
+            a["dg"], a["i"], a["g"], a["l"], a["al"], a["x"], a["w"], a["gc"], a["off"], a["S"],
+            a["dl"], a["dt"], a["T"], a["d"], a["E"], a["k"], 1, a["out"], a["dw"], a["db"],
+            a["dx"], 0, a["ws"], a["n"], None)
+
+    assert call(dt=5) == 2 and call(k=9) == 1 and call(d=60) == 1 and call(T=-1) == 1
+    assert call(S=2) == 1 and "seq_offsets" in _err(L)
+    assert call(S=0, off=p) == 1
+    assert call(dw=None, db=p) == 1 and "dbias" in _err(L)
+    for name in ("dg", "i", "g", "l", "x", "w", "gc", "ws"):
+        assert call(**{name: None}) == 1, name
+    for name in ("l", "x", "w", "dx", "out", "ws"):
+        assert call(**{name: p + 4}) == 1 and "aligned" in _err(L), name
+    assert call(n=need - 1) == 3
+
+
+def test_expert_backward_at_a_checkpoint_refusals(L):
+    keep, p = _fake()
+
+    def call(**kw):
+        a = dict(dict(dy=p, dout=None, gate=None, x=p, rs=p, T=10, k=2, q=p, sc=p, dt=1, d=128,
+                      f=128, R=20, dx=p, n=1 << 30), **kw)
+        return L.moe_grouped_ffn_bwd_gather_act8(
+            a["dy"], a["dout"], a["gate"], a["x"], a["rs"], a["T"], a["k"], a["q"], a["sc"], p, p,
+            p, None, a["dt"], 8, a["d"], a["f"], a["R"], a["dx"], p, p, 0, p, a["n"], None)
+
+    assert call(dt=0) == 2 and "LAEP_BF16" in _err(L)
+    assert call(d=96) == 2 and call(R=21) == 1 and call(rs=None) == 1
+    assert call(q=None) == 1 and call(sc=None) == 1 and call(dx=None) == 1
+    assert call(q=p + 4) == 1 and call(sc=p + 4) == 1 and "aligned" in _err(L)
+    assert call(dy=None) == 1 and "dout" in _err(L)
+    assert call(n=64) == 3 and "moe_grouped_ffn_bwd_gather_act8" in _err(L)
+    big = L.moe_grouped_ffn_bwd_gather_act8(None, p, p, p, p, 1 << 20, 1, p, p, p, p, p, None, 1, 8,
+                                            1024, 128, 20, p, p, p, 0, p, 1 << 40, None)
+    assert big == 2 and "2 GiB" in _err(L)
