@@ -274,3 +274,43 @@ def test_example_trains(act_bits):
     history = train_block.train(steps=12, act_bits=act_bits)
     assert all(np.isfinite(v).all() for v in history)
     assert history[-1][0] < 0.9 * history[0][0]
+
+
+def test_block_step_in_a_graph():
+    """A captured training step replays to the eager bits, with eager work between."""
+    T, d, E, k, f = 500, 128, 8, 2, 128
+    case("block step, graph replays")
+    g = torch.Generator(device="cuda").manual_seed(4)
+    r = lambda *s, std=1.0, dt=BF16: (std * torch.randn(s, generator=g, device="cuda")).to(dt)
+    w = laep.BlockWeights(1 + r(d, std=0.1, dt=F32), r(d, std=0.1, dt=F32), r(E, d, std=0.3),
+                          r(E, 2 * f, d, std=0.1), r(E, d, f, std=0.1))
+    off = torch.tensor([0, 100, 100, 500], dtype=torch.int32, device="cuda")
+    plan = laep.MoEBlockPlan(T, d, E, k, f, n_seq=3)
+    x, res, dout = r(T, d), r(T, d), r(T, d)
+
+    def step():
+        out, s = plan.forward(x, w, res, seq_offsets=off)
+        dx = plan.backward(dout, w, want_dbias=True)
+        p = plan.layer
+        return [out, s, dx, plan.loss, plan.seq_counts, plan.dgamma, plan.dbeta, p.dw_router,
+                p.dbias, p.dw_gate_up, p.dw_down]
+
+    def inputs(seed):
+        h = torch.Generator(device="cuda").manual_seed(seed)
+        for t in (x, res, dout):
+            t.copy_(torch.randn(t.shape, generator=h, device="cuda"))
+
+    step()                       # streams and buffers exist before the capture
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for seed in (10, 11, 12):
+        inputs(seed)
+        want = [t.clone() for t in step()]
+        for t in outs:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
