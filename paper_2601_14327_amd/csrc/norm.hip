@@ -14,14 +14,17 @@
 namespace laep {
 namespace {
 
-// 8 consecutive elements in their storage format
-template <typename T> struct Vec8;
-template <> struct Vec8<bf16_t> {
+// 16 bytes of consecutive elements in their storage format, N of them, so that the
+// lanes of a wave read and write one contiguous run (8 float32 columns a lane, two loads
+// 32 bytes apart, took 45 us instead of 40 for the backward of 4000 x 4096 float32)
+template <typename T> struct Vec;
+template <> struct Vec<bf16_t> {
+  static constexpr int N = 8;
   u32x4_t r;
   __device__ __forceinline__ void load(const bf16_t* p) {
     r = ld_stream(reinterpret_cast<const u32x4_t*>(p));
   }
-  __device__ __forceinline__ void get(float v[8]) const {
+  __device__ __forceinline__ void get(float v[N]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       v[2 * i] = lo_bf16(r[i]);
@@ -29,7 +32,7 @@ template <> struct Vec8<bf16_t> {
     }
   }
   // v rounded to storage, and widened again
-  __device__ __forceinline__ void put(float v[8]) {
+  __device__ __forceinline__ void put(float v[N]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
     get(v);
@@ -38,41 +41,49 @@ template <> struct Vec8<bf16_t> {
     st_stream(reinterpret_cast<u32x4_t*>(p), r);
   }
 };
-template <> struct Vec8<float> {
-  f32x4_t a, b;
+template <> struct Vec<float> {
+  static constexpr int N = 4;
+  f32x4_t r;
   __device__ __forceinline__ void load(const float* p) {
-    a = ld_stream(reinterpret_cast<const f32x4_t*>(p));
-    b = ld_stream(reinterpret_cast<const f32x4_t*>(p) + 1);
+    r = ld_stream(reinterpret_cast<const f32x4_t*>(p));
   }
-  __device__ __forceinline__ void get(float v[8]) const {
+  __device__ __forceinline__ void get(float v[N]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[i] = a[i];
-      v[4 + i] = b[i];
-    }
+    for (int i = 0; i < N; ++i) v[i] = r[i];
   }
-  __device__ __forceinline__ void put(float v[8]) {
-    a = f32x4_t{v[0], v[1], v[2], v[3]};
-    b = f32x4_t{v[4], v[5], v[6], v[7]};
-  }
+  __device__ __forceinline__ void put(float v[N]) { r = f32x4_t{v[0], v[1], v[2], v[3]}; }
   __device__ __forceinline__ void store(float* p) const {
-    st_stream(reinterpret_cast<f32x4_t*>(p), a);
-    st_stream(reinterpret_cast<f32x4_t*>(p) + 1, b);
+    st_stream(reinterpret_cast<f32x4_t*>(p), r);
   }
 };
+template <int N>
+__device__ __forceinline__ void load_f32(const float* p, float v[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const f32x4_t r = *reinterpret_cast<const f32x4_t*>(p + i);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[i + q] = r[q];
+  }
+}
 
-// A row belongs to NL lanes (a power of two), lane l holding the 8-column vectors
-// l, l + NL, ... (VPL of them), so it is read once; a workgroup of at least kFwdThreads
-// or kBwdThreads threads walks the rows, gamma, beta and, backwards, its columns' sums
+// A row belongs to NL lanes (a power of two), lane l holding the 16-byte vectors
+// l, l + NL, ... (VPL of them), so it is read once; a workgroup of a given number of
+// threads at least walks the rows, gamma, beta and, backwards, its columns' sums
 // staying in registers.  One vector a lane wherever 512 lanes hold the row: with two,
 // four or eight the forward took 210, 212 and 226 us against 195 at 32768 x 4096 bf16
-// with a residual.  Forward: 1024 workgroups of 256 threads, each row's loads issued
-// after the last one's stores: 179 us (6.0 TB/s of 6.2 that a copy reaches), 25 us at
-// 8192 x 2048; loading the next row ahead 196 and 29 us, a workgroup for every row 205
-// and 26.  Backward: 256 workgroups of 512 threads, since each writes a row of partial
-// sums, with the next row's loads ahead: 184 us (5.8 TB/s) at 32768 x 4096 with dres,
-// 30 us at 8192 x 2048; 256 threads 186 and 41, 512 workgroups 189 and 34.
-constexpr int kFwdThreads = 512, kBwdThreads = 512, kMaxLanes = 512;
+// with a residual.  Forward: 512 workgroups of 512 threads, each row's loads issued
+// after the last one's stores: 181 us (5.9 TB/s of 6.2 that a copy reaches), 24 us at
+// 8192 x 2048; loading the next row ahead 195 and 27 us, a workgroup for every row 205
+// and 26.  Backward: 256 workgroups, since each writes a row of partial sums, of 1024
+// threads while the registers last, with the next row's loads ahead: 174 us (6.2 TB/s)
+// at 32768 x 4096 bf16 with dres, 29 us at 8192 x 2048; 512 threads 179 and 29, two
+// rows ahead 172 and 29 there but 78 against 74 at 30000 x 1000 float32; 512
+// workgroups 195 and 31.
+constexpr int kFwdThreads = 512, kMaxLanes = 512;
+template <typename T>
+constexpr int bwd_threads(int vpl) {
+  return Vec<T>::N * vpl <= 8 ? 1024 : 512;
+}
 template <int NL, int MIN_NT> struct NormShape {
   static constexpr int NT = NL > MIN_NT ? NL : MIN_NT;
   static constexpr int ROWS = NT / NL;                   // rows at a time
@@ -91,32 +102,33 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
     const float* __restrict__ beta, unsigned n_rows, int d, float eps, T* sum_out, T* __restrict__ y,
     float* __restrict__ mean, float* __restrict__ rstd) {
   using S = NormShape<NL, kFwdThreads>;
+  constexpr int N = Vec<T>::N;
   __shared__ float s_red[2][S::NT / kWave][2];
-  const int nvec = d / 8;
+  const int nvec = d / N;
   const int l = threadIdx.x % NL, sub = threadIdx.x / NL;
   const int wave = threadIdx.x / kWave, wave0 = wave - wave % S::WAVES;
-  float g[VPL][8], b[VPL][8];
+  float g[VPL][N], b[VPL][N];
   int cols = 0;               // columns of this wave's part of a row
 #pragma unroll
   for (int u = 0; u < VPL; ++u) {
     const int v = l + u * NL;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) g[u][q] = b[u][q] = 0.0f;
+    for (int q = 0; q < N; ++q) g[u][q] = b[u][q] = 0.0f;
     if (v < nvec) {
-      Elem<float>::load8(gamma + (size_t)v * 8, g[u]);
-      if (beta) Elem<float>::load8(beta + (size_t)v * 8, b[u]);
+      load_f32<N>(gamma + (size_t)v * N, g[u]);
+      if (beta) load_f32<N>(beta + (size_t)v * N, b[u]);
     }
-    if (NL > kWave) cols += 8 * min(kWave, max(0, nvec - u * NL - (wave % S::WAVES) * kWave));
+    if (NL > kWave) cols += N * min(kWave, max(0, nvec - u * NL - (wave % S::WAVES) * kWave));
   }
   if (NL <= kWave) cols = d;
-  Vec8<T> xv[VPL], rv[VPL];
+  Vec<T> xv[VPL], rv[VPL];
   auto load = [&](unsigned row) {
 #pragma unroll
     for (int u = 0; u < VPL; ++u) {
       const int v = l + u * NL;
       if (row < n_rows && v < nvec) {
-        xv[u].load(x + (size_t)row * d + (size_t)v * 8);
-        if (residual) rv[u].load(residual + (size_t)row * d + (size_t)v * 8);
+        xv[u].load(x + (size_t)row * d + (size_t)v * N);
+        if (residual) rv[u].load(residual + (size_t)row * d + (size_t)v * N);
       }
     }
   };
@@ -126,25 +138,25 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
   for (int it = 0;; it ^= 1) {
     const bool more = n_rows - base > step;
     load(row);
-    float s[VPL][8];
+    float s[VPL][N];
     float sum = 0.0f;
 #pragma unroll
     for (int u = 0; u < VPL; ++u) {
       const int v = l + u * NL;
 #pragma unroll
-      for (int q = 0; q < 8; ++q) s[u][q] = 0.0f;
+      for (int q = 0; q < N; ++q) s[u][q] = 0.0f;
       if (row >= n_rows || v >= nvec) continue;
       xv[u].get(s[u]);
       if (residual) {
-        float r[8];
+        float r[N];
         rv[u].get(r);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) s[u][q] += r[q];
+        for (int q = 0; q < N; ++q) s[u][q] += r[q];
         xv[u].put(s[u]);
-        if (sum_out) xv[u].store(sum_out + (size_t)row * d + (size_t)v * 8);
+        if (sum_out) xv[u].store(sum_out + (size_t)row * d + (size_t)v * N);
       }
 #pragma unroll
-      for (int q = 0; q < 8; ++q) sum += s[u][q];
+      for (int q = 0; q < N; ++q) sum += s[u][q];
     }
     // the wave's own mean and centred squares; several waves' are merged by
     //   M2 = sum_w (M2_w + n_w (mu_w - mu)^2)
@@ -154,7 +166,7 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
     for (int u = 0; u < VPL; ++u)
       if (l + u * NL < nvec) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) sq += (s[u][q] - mu) * (s[u][q] - mu);
+        for (int q = 0; q < N; ++q) sq += (s[u][q] - mu) * (s[u][q] - mu);
       }
     sq = row_sum<NL>(sq);
     if constexpr (S::WAVES > 1) {
@@ -169,7 +181,7 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
       for (int w = 0; w < S::WAVES; ++w) {
         n[w] = 0;
 #pragma unroll
-        for (int u = 0; u < VPL; ++u) n[w] += 8 * min(kWave, max(0, nvec - u * NL - w * kWave));
+        for (int u = 0; u < VPL; ++u) n[w] += N * min(kWave, max(0, nvec - u * NL - w * kWave));
         tot += s_red[it][wave0 + w][0] * (float)n[w];
       }
       mu = tot / (float)d;
@@ -186,12 +198,12 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
       for (int u = 0; u < VPL; ++u) {
         const int v = l + u * NL;
         if (v >= nvec) continue;
-        float o[8];
+        float o[N];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) o[q] = (s[u][q] - mu) * rs * g[u][q] + b[u][q];
-        Vec8<T> ov;
+        for (int q = 0; q < N; ++q) o[q] = (s[u][q] - mu) * rs * g[u][q] + b[u][q];
+        Vec<T> ov;
         ov.put(o);
-        ov.store(y + (size_t)row * d + (size_t)v * 8);
+        ov.store(y + (size_t)row * d + (size_t)v * N);
       }
       if (l == 0) {
         if (mean) mean[row] = mu;
@@ -206,34 +218,35 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
 
 // dx of the rows a workgroup walks, and its rows' sums of dy xh and dy.
 template <typename T, int NL, int VPL>
-__global__ __launch_bounds__((NormShape<NL, kBwdThreads>::NT)) void norm_bwd_kernel(
+__global__ __launch_bounds__((NormShape<NL, bwd_threads<T>(VPL)>::NT)) void norm_bwd_kernel(
     const T* dy, const T* __restrict__ sv, const float* __restrict__ gamma,
     const float* __restrict__ mean, const float* __restrict__ rstd, const T* dres,
     unsigned n_rows, int d, T* dx, float* __restrict__ part) {
-  using S = NormShape<NL, kBwdThreads>;
-  // four vectors a lane leave no registers for the next row, nor for gamma
-  constexpr bool AHEAD = VPL <= 2;
+  using S = NormShape<NL, bwd_threads<T>(VPL)>;
+  constexpr int N = Vec<T>::N;
+  // 32 columns a lane leave no registers for the next row, nor for gamma
+  constexpr bool AHEAD = N * VPL <= 16;
   __shared__ float s_red[2][S::NT / kWave][2];
-  const int nvec = d / 8;
+  const int nvec = d / N;
   const int l = threadIdx.x % NL, sub = threadIdx.x / NL;
   const int wave = threadIdx.x / kWave, wave0 = wave - wave % S::WAVES;
-  float held[AHEAD ? VPL : 1][8], wg[VPL][8], wb[VPL][8];
+  float held[AHEAD ? VPL : 1][N], wg[VPL][N], wb[VPL][N];
 #pragma unroll
   for (int u = 0; u < VPL; ++u) {
     const int v = l + u * NL;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) wg[u][q] = wb[u][q] = 0.0f;
-    if (AHEAD && v < nvec) Elem<float>::load8(gamma + (size_t)v * 8, held[AHEAD ? u : 0]);
+    for (int q = 0; q < N; ++q) wg[u][q] = wb[u][q] = 0.0f;
+    if (AHEAD && v < nvec) load_f32<N>(gamma + (size_t)v * N, held[AHEAD ? u : 0]);
   }
-  auto gamma_of = [&](int u, float g[8]) {   // of a vector inside the row
+  auto gamma_of = [&](int u, float g[N]) {   // of a vector inside the row
     if constexpr (AHEAD) {
 #pragma unroll
-      for (int q = 0; q < 8; ++q) g[q] = held[u][q];
+      for (int q = 0; q < N; ++q) g[q] = held[u][q];
     } else {
-      Elem<float>::load8(gamma + (size_t)(l + u * NL) * 8, g);
+      load_f32<N>(gamma + (size_t)(l + u * NL) * N, g);
     }
   };
-  Vec8<T> xv[VPL], yv[VPL], rv[VPL];
+  Vec<T> xv[VPL], yv[VPL], rv[VPL];
   float mu = 0.0f, rs = 0.0f;
   auto load = [&](unsigned row) {
     if (row < n_rows) {
@@ -243,7 +256,7 @@ __global__ __launch_bounds__((NormShape<NL, kBwdThreads>::NT)) void norm_bwd_ker
 #pragma unroll
     for (int u = 0; u < VPL; ++u) {
       const int v = l + u * NL;
-      const size_t at = (size_t)row * d + (size_t)v * 8;
+      const size_t at = (size_t)row * d + (size_t)v * N;
       if (row < n_rows && v < nvec) {
         xv[u].load(sv + at);
         yv[u].load(dy + at);
@@ -260,21 +273,21 @@ __global__ __launch_bounds__((NormShape<NL, kBwdThreads>::NT)) void norm_bwd_ker
     if constexpr (!AHEAD) load(row);
     const bool on = row < n_rows;
     const float r1 = rs;
-    float xh[VPL][8], dv[VPL][8];
-    Vec8<T> res[VPL];
+    float xh[VPL][N], dv[VPL][N];
+    Vec<T> res[VPL];
     float a = 0.0f, b = 0.0f;
 #pragma unroll
     for (int u = 0; u < VPL; ++u) {
 #pragma unroll
-      for (int q = 0; q < 8; ++q) xh[u][q] = dv[u][q] = 0.0f;
+      for (int q = 0; q < N; ++q) xh[u][q] = dv[u][q] = 0.0f;
       if (!on || l + u * NL >= nvec) continue;
       xv[u].get(xh[u]);
       yv[u].get(dv[u]);
       if (AHEAD && dres) res[u] = rv[u];
-      float g[8];
+      float g[N];
       gamma_of(u, g);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
+      for (int q = 0; q < N; ++q) {
         xh[u][q] = (xh[u][q] - mu) * r1;
         a += g[q] * dv[u][q];
         b += g[q] * dv[u][q] * xh[u][q];
@@ -304,18 +317,18 @@ __global__ __launch_bounds__((NormShape<NL, kBwdThreads>::NT)) void norm_bwd_ker
     for (int u = 0; u < VPL; ++u) {
       const int v = l + u * NL;
       if (!on || v >= nvec) continue;
-      float o[8], r[8], g[8];
+      float o[N], r[N], g[N];
       gamma_of(u, g);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) o[q] = r1 * (g[q] * dv[u][q] - a - xh[u][q] * b);
+      for (int q = 0; q < N; ++q) o[q] = r1 * (g[q] * dv[u][q] - a - xh[u][q] * b);
       if (dres) {
         (AHEAD ? res[u] : rv[u]).get(r);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) o[q] += r[q];
+        for (int q = 0; q < N; ++q) o[q] += r[q];
       }
-      Vec8<T> ov;
+      Vec<T> ov;
       ov.put(o);
-      ov.store(dx + (size_t)row * d + (size_t)v * 8);
+      ov.store(dx + (size_t)row * d + (size_t)v * N);
     }
     if (!more) break;
     base += step;
@@ -324,7 +337,7 @@ __global__ __launch_bounds__((NormShape<NL, kBwdThreads>::NT)) void norm_bwd_ker
   if (!part) return;
   // rows side by side in the workgroup: their sums added in order through LDS
   float* const out = part + (size_t)blockIdx.x * 2 * d;
-  __shared__ float s_sum[S::ROWS > 1 ? S::ROWS * NL * 8 : 1];
+  __shared__ float s_sum[S::ROWS > 1 ? S::ROWS * NL * N : 1];
 #pragma unroll
   for (int u = 0; u < VPL; ++u)
 #pragma unroll
@@ -332,17 +345,22 @@ __global__ __launch_bounds__((NormShape<NL, kBwdThreads>::NT)) void norm_bwd_ker
       const float* const w = which ? wb[u] : wg[u];
       const int v = l + u * NL;
       if constexpr (S::ROWS == 1) {
-        if (v < nvec) Elem<float>::store8(out + which * d + (size_t)v * 8, w);
+        if (v < nvec) {
+#pragma unroll
+          for (int q = 0; q < N; q += 4)
+            *reinterpret_cast<f32x4_t*>(out + which * d + (size_t)v * N + q) =
+                f32x4_t{w[q], w[q + 1], w[q + 2], w[q + 3]};
+        }
       } else {
         __syncthreads();
 #pragma unroll
-        for (int q = 0; q < 8; ++q) s_sum[(sub * NL + l) * 8 + q] = w[q];
+        for (int q = 0; q < N; ++q) s_sum[(sub * NL + l) * N + q] = w[q];
         __syncthreads();
-        for (int c = threadIdx.x; c < NL * 8; c += S::NT) {
+        for (int c = threadIdx.x; c < NL * N; c += S::NT) {
           float t = 0.0f;
 #pragma unroll
-          for (int i = 0; i < S::ROWS; ++i) t += s_sum[i * NL * 8 + c];
-          const int col = u * NL * 8 + c;
+          for (int i = 0; i < S::ROWS; ++i) t += s_sum[i * NL * N + c];
+          const int col = u * NL * N + c;
           if (col < d) out[which * d + col] = t;
         }
       }
@@ -522,13 +540,17 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_wide_kernel(
 }
 
 // workgroups of a call: forward, backward (each of these writes its partial sums)
-constexpr int kFwdGroups = 512, kBwdGroups = 256;
+// Without a residual a row brings half the loads, and three workgroups a CU do better
+// than two: 32768 x 4096 bf16 104 us for 121, 8192 x 2048 15.0 / 17.4, 30000 x 1000
+// float32 47 / 57; with one, two: 181 for 187, 24.3 / 24.4, 4000 x 4096 float32 47 / 52.
+constexpr int kFwdGroups = 512, kFwdGroupsAlone = 768, kBwdGroups = 256;
 
-// f(lanes per row, vectors per lane) for rows of nvec vectors: one vector a lane
-// while 512 lanes hold the row, then two or four; false past that.
-template <typename F>
-bool norm_shape(int nvec, F f) {
+// f(lanes per row, vectors per lane) for rows of d columns: one vector a lane while 512
+// lanes hold the row, then two, four and so on up to 32 columns; false past that.
+template <typename T, typename F>
+bool norm_shape(int d, F f) {
   using std::integral_constant;
+  const int nvec = d / Vec<T>::N;
   const integral_constant<int, 1> one{};
   const integral_constant<int, kMaxLanes> most{};
   if (nvec <= 8) f(integral_constant<int, 8>{}, one);
@@ -540,6 +562,8 @@ bool norm_shape(int nvec, F f) {
   else if (nvec <= kMaxLanes) f(most, one);
   else if (nvec <= 2 * kMaxLanes) f(most, integral_constant<int, 2>{});
   else if (nvec <= 4 * kMaxLanes) f(most, integral_constant<int, 4>{});
+  else if (Vec<T>::N == 4 && nvec <= 8 * kMaxLanes)
+    f(most, integral_constant<int, Vec<T>::N == 4 ? 8 : 4>{});
   else return false;
   return true;
 }
@@ -558,12 +582,12 @@ template <typename T>
 hipError_t norm_fwd_t(const T* x, const T* residual, const float* gamma, const float* beta, int n,
                       int d, float eps, T* sum_out, T* y, float* mean, float* rstd,
                       hipStream_t s) {
-  const bool fits = norm_shape(d / 8, [&](auto nl, auto vpl) {
+  const bool fits = norm_shape<T>(d, [&](auto nl, auto vpl) {
     constexpr int NL = decltype(nl)::value, VPL = decltype(vpl)::value;
     using S = NormShape<NL, kFwdThreads>;
-    const int need = (n - 1) / S::ROWS + 1;
+    const int need = (n - 1) / S::ROWS + 1, most = residual ? kFwdGroups : kFwdGroupsAlone;
     hipLaunchKernelGGL((norm_fwd_kernel<T, NL, VPL>),
-                       dim3((unsigned)(need < kFwdGroups ? need : kFwdGroups)), dim3(S::NT), 0, s,
+                       dim3((unsigned)(need < most ? need : most)), dim3(S::NT), 0, s,
                        x, residual, gamma, beta, n, d, eps, sum_out, y, mean, rstd);
   });
   if (!fits)
@@ -594,9 +618,9 @@ hipError_t norm_bwd_t(const T* dy, const T* sv, const float* gamma, const float*
                       const float* rstd, const T* dres, int n, int d, T* dx, float* dgamma,
                       float* dbeta, float* part, hipStream_t s) {
   int grid = 0;
-  const bool fits = n == 0 || norm_shape(d / 8, [&](auto nl, auto vpl) {
+  const bool fits = n == 0 || norm_shape<T>(d, [&](auto nl, auto vpl) {
     constexpr int NL = decltype(nl)::value, VPL = decltype(vpl)::value;
-    using S = NormShape<NL, kBwdThreads>;
+    using S = NormShape<NL, bwd_threads<T>(VPL)>;
     const int need = (n - 1) / S::ROWS + 1;
     grid = need < kBwdGroups ? need : kBwdGroups;
     hipLaunchKernelGGL((norm_bwd_kernel<T, NL, VPL>), dim3((unsigned)grid), dim3(S::NT), 0, s, dy,
