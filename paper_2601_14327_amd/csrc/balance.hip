@@ -111,18 +111,27 @@ __device__ __forceinline__ int first_seq(const int32_t* __restrict__ off, int n_
   return lo;
 }
 
-// Four experts of a row, 4 l .. 4 l + 3; VEC: E is a multiple of four.  Streaming loads:
+// Four experts of a row, 4 l .. 4 l + 3, of a lane whose first is one.  Streaming loads:
 // what the caches hold is still found there, and the rest does not push out what other
-// calls wrote (131072 x 256, first pass: 43 -> 28 us).
+// calls wrote (131072 x 256, first pass: 43 -> 28 us).  VEC: E is a multiple of four and
+// rows are 16-byte aligned; else a lane's four are loaded together all the same, 4-byte
+// aligned, the last lane's from the row's last four and shifted (131072 tokens trained,
+// four single loads / one: 45 experts 39 / 30 us, 131 100 / 77, 250 161 / 97).
+typedef f32x4_t f32x4_a4_t __attribute__((aligned(4)));
 template <bool VEC>
 __device__ __forceinline__ void load4(const float* __restrict__ row, int e0, int E, float v[4]) {
-  if constexpr (VEC) {
-    const f32x4_t r = ld_stream(reinterpret_cast<const f32x4_t*>(row + e0));
+  if (VEC || E >= 4) {
+    const int at = VEC ? e0 : min(e0, E - 4), shift = e0 - at;
+    f32x4_t r;
+    if constexpr (VEC) r = ld_stream(reinterpret_cast<const f32x4_t*>(row + at));
+    else r = __builtin_nontemporal_load(reinterpret_cast<const f32x4_a4_t*>(row + at));
+    if (!VEC && (shift & 1)) r = f32x4_t{r[1], r[2], r[3], r[3]};
+    if (!VEC && (shift & 2)) r = f32x4_t{r[2], r[3], r[3], r[3]};
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = r[i];
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = e0 + i < E ? __builtin_nontemporal_load(row + e0 + i) : 0.0f;
+    for (int i = 0; i < 4; ++i) v[i] = e0 + i < E ? row[e0 + i] : 0.0f;
   }
 }
 
@@ -247,7 +256,7 @@ __global__ __launch_bounds__(kBalThreads) void balance_chunk_kernel(
         const int row = r + u * ROWS + first;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[u][i] = -INFINITY;
-        if (row < b - a && (!VEC || e0 < E))
+        if (row < b - a && e0 < E)
           load4<VEC>(logits + (size_t)(a + row) * E, e0, E, v[u]);
       }
 #pragma unroll
@@ -377,6 +386,10 @@ __global__ __launch_bounds__(kBalThreads) void balance_bwd_kernel(
       f32x4_t r = {v[0], v[1], v[2], v[3]};
       if (accumulate) r += *reinterpret_cast<f32x4_t*>(d);
       *reinterpret_cast<f32x4_t*>(d) = r;
+    } else if (e0 + 4 <= E) {
+      f32x4_t r = {v[0], v[1], v[2], v[3]};
+      if (accumulate) r += *reinterpret_cast<f32x4_a4_t*>(d);
+      *reinterpret_cast<f32x4_a4_t*>(d) = r;
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -408,7 +421,7 @@ __global__ __launch_bounds__(kBalThreads) void balance_bwd_kernel(
         const int row = r + u * ROWS + first;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[u][i] = -INFINITY;
-        if (row < b - a && (!VEC || e0 < E))
+        if (row < b - a && e0 < E)
           load4<VEC>(logits + (size_t)(a + row) * E, e0, E, v[u]);
       }
 #pragma unroll
