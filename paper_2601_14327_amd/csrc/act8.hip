@@ -15,7 +15,7 @@ namespace laep {
 namespace {
 
 // HBM-bound; one vector of 8 columns a thread and no loop while the grid allows: 16
-// columns a thread took 178 us and persistent grids of 1024 to 4096 workgroups 146 to
+// columns a thread took 178 us and persistent grids of 1024 to 4096 workgroups 144 to
 // 160 us against 132 (6.1 TB/s) for save and load of 65536 x 2048 bf16.  Stores stream:
 // what they write is read much later, or by a product that reads it many times
 // (ordinary ones: 141 us, and 122 against 111 in the SwiGLU backward at d_ff 1024).

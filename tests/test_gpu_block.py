@@ -233,6 +233,18 @@ def test_balance_loss(T, E, k, S, dead):
     _check_balance_bwd(logits, alive, off, got[3], acc, -3.0, base.astype(np.float64))
 
 
+@pytest.mark.parametrize("E", [3, 45, 64, 253])
+def test_balance_gradient_in_place(E):
+    T, k = 1500, 1
+    case(f"balance gradient over the logits E={E}")
+    logits, idx, _, off = _balance_inputs(T, E, k, 3, 0, E)
+    lt, ot = dev(logits, F32), dev(off, torch.int32)
+    grad = laep.moe_balance_loss(lt, dev(idx, torch.int32), seq_offsets=ot)[3]
+    want = laep.moe_balance_loss_bwd(lt, grad, seq_offsets=ot)
+    got = laep.moe_balance_loss_bwd(lt, grad, seq_offsets=ot, dlogits=lt)
+    assert got is lt and torch.equal(got, want)
+
+
 def test_balance_counts_match_the_layer():
     T, E, k = 1000, 64, 8
     case("balance loss, counts of a routed batch")
