@@ -81,7 +81,7 @@ def _check_norm_bwd(x, dy, gamma, mean, rstd, dres, dtype, out):
 
 
 NORM_SIZES = [(1, 8), (3, 16), (5, 72), (64, 128), (1, 2048), (257, 504), (65, 1000), (33, 2048),
-              (130, 2056), (17, 4096), (9, 4104), (5, 8192), (3, 16392), (1200, 256), (2500, 64)]
+              (130, 2056), (16, 2048), (17, 2048), (8, 4096), (17, 4096), (9, 4104), (5, 8192), (3, 16392), (1200, 256), (2500, 64)]
 
 
 @pytest.mark.parametrize("T,d", NORM_SIZES)
@@ -209,7 +209,8 @@ def _check_balance_bwd(logits, alive, off, grad, got, dloss=1.0, add=0.0):
 BALANCE = [(1, 1, 1, 1, 0), (1, 64, 8, 1, 0), (3, 2, 1, 1, 0), (8, 64, 8, 1, 0), (8, 64, 8, 5, 0),
            (63, 5, 2, 1, 0), (64, 8, 2, 3, 2), (65, 45, 8, 4, 0), (200, 33, 4, 1, 8),
            (129, 256, 8, 7, 64), (1000, 16, 2, 1, 0), (777, 100, 3, 40, 25), (513, 128, 8, 2, 0),
-           (300, 255, 4, 1, 1), (2100, 64, 8, 1, 0), (5000, 7, 2, 33, 0), (4099, 64, 2, 600, 5)]
+           (300, 255, 4, 1, 1), (128, 256, 4, 4, 0), (129, 256, 4, 4, 0),
+           (512, 64, 8, 2, 8), (513, 64, 8, 2, 8), (8192, 4, 1, 3, 0), (2100, 64, 8, 1, 0), (5000, 7, 2, 33, 0), (4099, 64, 2, 600, 5)]
 
 
 @pytest.mark.parametrize("T,E,k,S,dead", BALANCE)
