@@ -3,8 +3,8 @@ NumPy): layer norm, the router's balance loss, 8-bit activation checkpoints.
 
 Test infrastructure only; see the package docstring.
 
-The paper names no norm and uses balance losses only in its comparison
-systems; the readings used here:
+Only the paper's comparison systems train with a balance loss, and its block's
+norm is not spelled out; the readings used here:
 
 * layer norm over the columns of s = round(x + residual), the variance the mean
   of the centred squares, statistics unrounded;
