@@ -31,7 +31,7 @@ extern "C" {
  *   sum_out   device [T, d_model] dtype or NULL; needs a residual; may be x or
  *             residual (the residual stream updated in place)
  *   mean, rstd  device [T] float32 or NULL (the backward pass needs both)
- *   d_model % 8 == 0, T >= 0.  y must not overlap the inputs or sum_out.
+ *   d_model % 8 == 0 and at most 2^28, T >= 0.  y must not overlap the inputs or sum_out.
  */
 int moe_layer_norm(const void* x, const void* residual, const float* gamma,
                    const float* beta, int dtype, int T, int d_model, float eps,
@@ -154,7 +154,11 @@ int moe_route_bwd_balance(const float* dgate, const int32_t* topk_idx,
 int moe_act8_save(const void* act, int dtype, int64_t R, int C, int8_t* q,
                   uint8_t* scale, void* stream);
 
-/* moe_act8_load -- act[r, c] = q[r, c] * 2^(scale[r, c / 32] - 127), in dtype. */
+/*
+ * moe_act8_load -- act[r, c] = q[r, c] * 2^(scale[r, c / 32] - 127), in dtype;
+ * NaN where the scale is 255.  q and scale as moe_act8_save writes them
+ * (scale 1 to 255).
+ */
 int moe_act8_load(const int8_t* q, const uint8_t* scale, int dtype, int64_t R,
                   int C, void* act, void* stream);
 

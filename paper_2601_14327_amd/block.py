@@ -81,7 +81,8 @@ class MoEBlockPlan:
 
     def forward(self, x, weights: BlockWeights, residual=None, *, bias=None, alive=None,
                 seq_offsets=None, expert_map=None, etn_accum=None):
-        """Returns (out, s).  ``alive``: the router's mask of unpruned experts;
+        """Returns (out, s); without a residual s is x, which must then keep its values
+        until the backward pass.  ``alive``: the router's mask of unpruned experts;
         ``seq_offsets``: int32 [n_seq + 1] on the device, with n_seq > 1."""
         p = self.layer
         y, s, _, _ = api.moe_layer_norm(x, weights.gamma, weights.beta, residual=residual,

@@ -695,13 +695,29 @@ int moe_permute_bwd(const void* dx_perm, const int32_t* dest_row, int T, int k, 
                     "moe_permute_bwd");
 }
 
+}  // extern "C"
+
+namespace {
+
+// rows of a layer norm: column counts stay far inside int32, twice over
+int check_norm_rows(const char* name, int dtype, int T, int d_model) {
+  int rc = check_dtype(dtype);
+  if (rc) return rc;
+  if ((rc = check_rows(T, 1, d_model))) return rc;
+  REQUIRE(d_model <= 1 << 28, LAEP_ERR_UNSUPPORTED, "%s: d_model=%d exceeds 2^28", name, d_model);
+  return LAEP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
 // ---- the block around the experts (laep_block.h) ----------------------------------
 int moe_layer_norm(const void* x, const void* residual, const float* gamma, const float* beta,
                    int dtype, int T, int d_model, float eps, void* sum_out, void* y, float* mean,
                    float* rstd, void* stream) {
-  int rc = check_dtype(dtype);
+  int rc = check_norm_rows("moe_layer_norm", dtype, T, d_model);
   if (rc) return rc;
-  if ((rc = check_rows(T, 1, d_model))) return rc;
   REQUIRE(eps >= 0.0f && std::isfinite(eps), LAEP_ERR_INVALID_ARG,
           "moe_layer_norm: eps=%g must be finite and >= 0", (double)eps);
   REQUIRE(residual || !sum_out, LAEP_ERR_INVALID_ARG,
@@ -723,9 +739,8 @@ int moe_layer_norm_bwd(const void* dy, const void* s, const float* gamma, const 
                        const float* rstd, const void* dres, int dtype, int T, int d_model,
                        void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
                        void* stream) {
-  int rc = check_dtype(dtype);
+  int rc = check_norm_rows("moe_layer_norm_bwd", dtype, T, d_model);
   if (rc) return rc;
-  if ((rc = check_rows(T, 1, d_model))) return rc;
   REQUIRE(dgamma || !dbeta, LAEP_ERR_INVALID_ARG,
           "moe_layer_norm_bwd: dbeta needs dgamma (they are computed together)");
   REQUIRE(aligned16(dgamma) && aligned16(dbeta), LAEP_ERR_INVALID_ARG,

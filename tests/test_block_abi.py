@@ -23,6 +23,7 @@ def test_layer_norm_refusals(L):
     assert fwd(dt=2) == 2 and "dtype" in _err(L)
     assert fwd(d=12) == 1 and "multiple of 8" in _err(L)
     assert fwd(d=0) == 1 and fwd(T=-1) == 1
+    assert fwd(d=(1 << 28) + 8) == 2 and "2^28" in _err(L)
     assert fwd(eps=-1.0) == 1 and fwd(eps=math.nan) == 1 and "eps" in _err(L)
     assert fwd(s=q) == 1 and "residual" in _err(L)
     assert fwd(x=None) == 1 and fwd(g=None) == 1 and fwd(y=None) == 1
@@ -159,6 +160,13 @@ def test_binding_refuses_on_the_device():
     idx = z(4, 2, dt=torch.int32)
     with pytest.raises(ValueError, match="topk_idx"):
         laep.moe_balance_loss(z(4, 8), idx.long())
+    with pytest.raises(ValueError, match="contiguous"):
+        laep.moe_balance_loss(z(8, 4).t(), idx)
+    with pytest.raises(ValueError, match="contiguous"):
+        laep.moe_act8_save(z(64, 4, dt=bf).t())
+    with pytest.raises(ValueError, match="contiguous"):
+        laep.moe_swiglu_bwd_act8(z(4, 64, dt=torch.int8), z(4, 2, dt=torch.uint8),
+                                 z(32, 4, dt=bf).t())
     with pytest.raises(ValueError, match="seq_offsets"):
         laep.moe_balance_loss(z(4, 8), idx, seq_offsets=z(3, dt=torch.int64))
     with pytest.raises(ValueError, match="grad_coef"):
