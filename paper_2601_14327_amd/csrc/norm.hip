@@ -66,27 +66,31 @@ __device__ __forceinline__ void load_f32(const float* p, float v[N]) {
   }
 }
 
-// A row belongs to NL lanes (a power of two), lane l holding the 16-byte vectors
-// l, l + NL, ... (VPL of them), so it is read once; a workgroup of a given number of
-// threads at least walks the rows, gamma, beta and, backwards, its columns' sums
-// staying in registers.  One vector a lane wherever 512 lanes hold the row: with two,
-// four or eight the forward took 210, 212 and 226 us against 195 at 32768 x 4096 bf16
-// with a residual.  Forward: 512 workgroups of 512 threads, each row's loads issued
-// after the last one's stores: 181 us (5.9 TB/s of 6.2 that a copy reaches), 24 us at
-// 8192 x 2048; loading the next row ahead 195 and 27 us, a workgroup for every row 205
-// and 26.  Backward: 256 workgroups, since each writes a row of partial sums, of 1024
-// threads while the registers last, with the next row's loads ahead: 174 us (6.2 TB/s)
-// at 32768 x 4096 bf16 with dres, 29 us at 8192 x 2048; 512 threads 179 and 29, two
-// rows ahead 172 and 29 there but 78 against 74 at 30000 x 1000 float32; 512
-// workgroups 195 and 31.
-constexpr int kFwdThreads = 512, kMaxLanes = 512;
-template <typename T>
-constexpr int bwd_threads(int vpl) {
-  return Vec<T>::N * vpl <= 8 ? 1024 : 512;
-}
-template <int NL, int MIN_NT> struct NormShape {
-  static constexpr int NT = NL > MIN_NT ? NL : MIN_NT;
-  static constexpr int ROWS = NT / NL;                   // rows at a time
+// A row belongs to NL lanes, lane l holding the 16-byte vectors l, l + NL, ... (VPL of
+// them), so it is read once; a workgroup walks the rows, several side by side where they
+// are short, gamma, beta and, backwards, its columns' sums staying in registers.  NL is a
+// power of two inside a wave, then the whole waves that hold the row (pairs of waves past
+// 512 lanes) up to 1024 lanes, and only past those a lane holds more than one vector: a
+// power of two leaves lanes idle (29392 x 2240 bf16 with a residual 110 us on 512 lanes,
+// 90 on 320), and two vectors a lane have fewer loads in flight (8192 x 5120 bf16 75 us
+// on 512 lanes, 57 on 640).
+// Every lane loads, those past the row or the rows the last one's bytes, which they do not
+// use: with a branch round the loads the compiler cannot tell which are pending where the
+// paths join, and waits for the stores as well (8192 x 5120 69 us for 57, 3000 x 10240 58
+// for 49).
+// Forward with a residual: workgroups for 20 waves a CU, each row's loads issued after
+// the last one's stores: 181 us at 32768 x 4096 bf16 (5.9 TB/s of 6.2 that a copy
+// reaches), 24 us at 8192 x 2048; loading the next row ahead 202 and 27, a workgroup for
+// every row 205 and 26.  Without one a row has half the loads, and the next row's go
+// ahead of this row's sums: 8192 x 2048 14.6 us for 15.1, 4000 x 5120 float32 34 for 41.
+// Backward: 256 workgroups, since each writes a row of partial sums, of up to 1024
+// threads, with the next row's loads ahead: 174 us (6.2 TB/s) at 32768 x 4096 bf16 with
+// dres, 28 us at 8192 x 2048; 512 threads 179 and 29, two rows ahead 172 and 29 there but
+// 78 against 74 at 30000 x 1000 float32; 512 workgroups 195 and 31.
+constexpr int kFwdThreads = 512, kBwdThreads = 1024, kMaxLanes = 1024;
+template <int NL, int MOST> struct NormShape {
+  static constexpr int ROWS = NL < MOST ? MOST / NL : 1;     // rows at a time
+  static constexpr int NT = ROWS * NL;
   static constexpr int WAVES = NL > kWave ? NL / kWave : 1;  // waves of a row
 };
 
@@ -96,7 +100,7 @@ __device__ __forceinline__ float row_sum(float v) {
   return lanes_sum<(NL < kWave ? NL : kWave)>(v);
 }
 
-template <typename T, int NL, int VPL>
+template <typename T, int NL, int VPL, bool RES>
 __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_kernel(
     const T* x, const T* residual, const float* __restrict__ gamma,
     const float* __restrict__ beta, unsigned n_rows, int d, float eps, T* sum_out, T* __restrict__ y,
@@ -125,19 +129,19 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
   auto load = [&](unsigned row) {
 #pragma unroll
     for (int u = 0; u < VPL; ++u) {
-      const int v = l + u * NL;
-      if (row < n_rows && v < nvec) {
-        xv[u].load(x + (size_t)row * d + (size_t)v * N);
-        if (residual) rv[u].load(residual + (size_t)row * d + (size_t)v * N);
-      }
+      const int v = min(l + u * NL, nvec - 1);
+      const size_t at = (size_t)min(row, n_rows - 1) * d + (size_t)v * N;
+      xv[u].load(x + at);
+      if (RES) rv[u].load(residual + at);
     }
   };
   const unsigned step = gridDim.x * S::ROWS;
   unsigned row = blockIdx.x * S::ROWS + sub;
+  if (!RES) load(row);
   unsigned base = blockIdx.x * S::ROWS;   // < n_rows; rows and steps may pass int32
   for (int it = 0;; it ^= 1) {
     const bool more = n_rows - base > step;
-    load(row);
+    if (RES) load(row);
     float s[VPL][N];
     float sum = 0.0f;
 #pragma unroll
@@ -147,7 +151,7 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
       for (int q = 0; q < N; ++q) s[u][q] = 0.0f;
       if (row >= n_rows || v >= nvec) continue;
       xv[u].get(s[u]);
-      if (residual) {
+      if (RES) {
         float r[N];
         rv[u].get(r);
 #pragma unroll
@@ -158,6 +162,7 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
 #pragma unroll
       for (int q = 0; q < N; ++q) sum += s[u][q];
     }
+    if (!RES && more) load(row + step);
     // the wave's own mean and centred squares; several waves' are merged by
     //   M2 = sum_w (M2_w + n_w (mu_w - mu)^2)
     float mu = cols ? row_sum<NL>(sum) / (float)cols : 0.0f;
@@ -218,15 +223,17 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
 
 // dx of the rows a workgroup walks, and its rows' sums of dy xh and dy.
 template <typename T, int NL, int VPL>
-__global__ __launch_bounds__((NormShape<NL, bwd_threads<T>(VPL)>::NT)) void norm_bwd_kernel(
+__global__ __launch_bounds__((NormShape<NL, kBwdThreads>::NT)) void norm_bwd_kernel(
     const T* dy, const T* __restrict__ sv, const float* __restrict__ gamma,
     const float* __restrict__ mean, const float* __restrict__ rstd, const T* dres,
     unsigned n_rows, int d, T* dx, float* __restrict__ sum_g, float* __restrict__ sum_b,
     int sum_stride) {
-  using S = NormShape<NL, bwd_threads<T>(VPL)>;
+  using S = NormShape<NL, kBwdThreads>;
   constexpr int N = Vec<T>::N;
-  // 32 columns a lane leave no registers for the next row, nor for gamma
-  constexpr bool AHEAD = N * VPL <= 16;
+  // The next row, and gamma, in registers while these last: 16 columns a lane only with
+  // up to 768 threads (3000 x 12288 bf16 61 us for 73; at 2000 x 14336, 896 threads, 78
+  // for 58, and 2000 x 12288 float32, four vectors, 96 for 85).
+  constexpr bool AHEAD = N * VPL <= 8 || (VPL == 2 && NL <= 768);
   __shared__ float s_red[2][S::NT / kWave][2];
   const int nvec = d / N;
   const int l = threadIdx.x % NL, sub = threadIdx.x / NL;
@@ -250,19 +257,15 @@ __global__ __launch_bounds__((NormShape<NL, bwd_threads<T>(VPL)>::NT)) void norm
   Vec<T> xv[VPL], yv[VPL], rv[VPL];
   float mu = 0.0f, rs = 0.0f;
   auto load = [&](unsigned row) {
-    if (row < n_rows) {
-      mu = mean[row];
-      rs = rstd[row];
-    }
+    row = min(row, n_rows - 1);
+    mu = mean[row];
+    rs = rstd[row];
 #pragma unroll
     for (int u = 0; u < VPL; ++u) {
-      const int v = l + u * NL;
-      const size_t at = (size_t)row * d + (size_t)v * N;
-      if (row < n_rows && v < nvec) {
-        xv[u].load(sv + at);
-        yv[u].load(dy + at);
-        if (dres) rv[u].load(dres + at);
-      }
+      const size_t at = (size_t)row * d + (size_t)min(l + u * NL, nvec - 1) * N;
+      xv[u].load(sv + at);
+      yv[u].load(dy + at);
+      if (dres) rv[u].load(dres + at);
     }
   };
   const unsigned step = gridDim.x * S::ROWS;
@@ -543,33 +546,45 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_wide_kernel(
   }
 }
 
-// workgroups of a call: forward, backward (each of these writes its partial sums)
-// Without a residual a row brings half the loads, and three workgroups a CU do better
-// than two: 32768 x 4096 bf16 104 us for 121, 8192 x 2048 15.0 / 17.4, 30000 x 1000
-// float32 47 / 57; with one, two: 181 for 187, 24.3 / 24.4, 4000 x 4096 float32 47 / 52.
-constexpr int kFwdGroups = 512, kFwdGroupsAlone = 768, kBwdGroups = 256;
+// Workgroups of a call.  Forward: waves a CU with a residual and without one: with it 24
+// take 188 us for 181 at 32768 x 4096 bf16, 86 for 81 at 30000 x 1000 float32, though 39
+// for 42 at 40000 x 640 bf16; without, 16 take 34 us for 28 at 24607 x 768 float32, 16 for
+// 15 at 8192 x 2048 bf16, and 32 take 64 for 56 at 29392 x 2240.
+constexpr int kCus = 256, kFwdWaves = 20, kFwdWavesAlone = 24, kBwdGroups = 256;
 
-// f(lanes per row, vectors per lane) for rows of d columns: one vector a lane while 512
-// lanes hold the row, then two, four and so on up to 32 columns; false past that.
+// f(lanes per row, vectors per lane) for rows of d columns; false past 16384.
 template <typename T, typename F>
 bool norm_shape(int d, F f) {
-  using std::integral_constant;
   const int nvec = d / Vec<T>::N;
-  const integral_constant<int, 1> one{};
-  const integral_constant<int, kMaxLanes> most{};
-  if (nvec <= 8) f(integral_constant<int, 8>{}, one);
-  else if (nvec <= 16) f(integral_constant<int, 16>{}, one);
-  else if (nvec <= 32) f(integral_constant<int, 32>{}, one);
-  else if (nvec <= 64) f(integral_constant<int, 64>{}, one);
-  else if (nvec <= 128) f(integral_constant<int, 128>{}, one);
-  else if (nvec <= 256) f(integral_constant<int, 256>{}, one);
-  else if (nvec <= kMaxLanes) f(most, one);
-  else if (nvec <= 2 * kMaxLanes) f(most, integral_constant<int, 2>{});
-  else if (nvec <= 4 * kMaxLanes) f(most, integral_constant<int, 4>{});
-  else if (Vec<T>::N == 4 && nvec <= 8 * kMaxLanes)
-    f(most, integral_constant<int, Vec<T>::N == 4 ? 8 : 4>{});
-  else return false;
-  return true;
+  const auto with = [&](auto nl, auto vpl) { return f(nl, vpl), true; };
+  const std::integral_constant<int, 1> one{};
+  if (nvec <= 8) return with(std::integral_constant<int, 8>{}, one);
+  if (nvec <= 16) return with(std::integral_constant<int, 16>{}, one);
+  if (nvec <= 32) return with(std::integral_constant<int, 32>{}, one);
+  switch ((nvec + kWave - 1) / kWave) {
+    case 1: return with(std::integral_constant<int, 64>{}, one);
+    case 2: return with(std::integral_constant<int, 128>{}, one);
+    case 3: return with(std::integral_constant<int, 192>{}, one);
+    case 4: return with(std::integral_constant<int, 256>{}, one);
+    case 5: return with(std::integral_constant<int, 320>{}, one);
+    case 6: return with(std::integral_constant<int, 384>{}, one);
+    case 7: return with(std::integral_constant<int, 448>{}, one);
+    case 8: return with(std::integral_constant<int, 512>{}, one);
+  }
+  const auto wide = [&](auto vpl) {
+    constexpr int TWO = 2 * kWave * decltype(vpl)::value;   // two waves' vectors
+    switch ((nvec + TWO - 1) / TWO) {
+      case 5: return with(std::integral_constant<int, 640>{}, vpl);
+      case 6: return with(std::integral_constant<int, 768>{}, vpl);
+      case 7: return with(std::integral_constant<int, 896>{}, vpl);
+      default: return with(std::integral_constant<int, kMaxLanes>{}, vpl);
+    }
+  };
+  if (nvec <= kMaxLanes) return wide(one);
+  if (nvec <= 2 * kMaxLanes) return wide(std::integral_constant<int, 2>{});
+  if (Vec<T>::N == 4 && nvec <= 4 * kMaxLanes)
+    return wide(std::integral_constant<int, Vec<T>::N == 4 ? 4 : 2>{});
+  return false;
 }
 
 inline int norm_parts(int T) { return T < kBwdGroups ? T : kBwdGroups; }
@@ -589,10 +604,14 @@ hipError_t norm_fwd_t(const T* x, const T* residual, const float* gamma, const f
   const bool fits = norm_shape<T>(d, [&](auto nl, auto vpl) {
     constexpr int NL = decltype(nl)::value, VPL = decltype(vpl)::value;
     using S = NormShape<NL, kFwdThreads>;
-    const int need = (n - 1) / S::ROWS + 1, most = residual ? kFwdGroups : kFwdGroupsAlone;
-    hipLaunchKernelGGL((norm_fwd_kernel<T, NL, VPL>),
-                       dim3((unsigned)(need < most ? need : most)), dim3(S::NT), 0, s,
-                       x, residual, gamma, beta, n, d, eps, sum_out, y, mean, rstd);
+    const int need = (n - 1) / S::ROWS + 1;
+    const auto run = [&](auto kernel, int waves) {
+      const int per = waves / (S::NT / kWave), most = kCus * (per > 1 ? per : 1);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(need < most ? need : most)), dim3(S::NT), 0, s, x,
+                         residual, gamma, beta, n, d, eps, sum_out, y, mean, rstd);
+    };
+    if (residual) run(norm_fwd_kernel<T, NL, VPL, true>, kFwdWaves);
+    else run(norm_fwd_kernel<T, NL, VPL, false>, kFwdWavesAlone);
   });
   if (!fits)
     hipLaunchKernelGGL(norm_fwd_wide_kernel<T>, dim3((unsigned)(n < kWideGroups ? n : kWideGroups)),
@@ -625,7 +644,7 @@ hipError_t norm_bwd_t(const T* dy, const T* sv, const float* gamma, const float*
   bool done = false;
   const bool fits = n == 0 || norm_shape<T>(d, [&](auto nl, auto vpl) {
     constexpr int NL = decltype(nl)::value, VPL = decltype(vpl)::value;
-    using S = NormShape<NL, bwd_threads<T>(VPL)>;
+    using S = NormShape<NL, kBwdThreads>;
     const int need = (n - 1) / S::ROWS + 1;
     grid = need < kBwdGroups ? need : kBwdGroups;
     // Up to four passes of its rows one workgroup takes them all: its sums are the

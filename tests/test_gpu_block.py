@@ -103,6 +103,32 @@ def test_layer_norm(T, d, dtype):
     assert torch.equal(dx, got[0])
 
 
+# widths of every number of waves a row may have, the last one partly filled; rows enough
+# that a workgroup walks several
+NORM_WIDTHS = [(1300, 776), (1300, 1224), (1300, 1496), (1300, 1544), (1300, 2504), (1300, 3000),
+               (1300, 3528), (600, 5112), (600, 6000), (600, 7160), (300, 9000), (300, 12000),
+               (300, 14000), (300, 15000), (1, 5112), (2, 14000)]
+
+
+@pytest.mark.parametrize("T,d", NORM_WIDTHS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_layer_norm_widths(T, d, dtype):
+    case(f"layer norm T={T} d={d} {dtype}")
+    x, res, dy, gamma, beta = _norm_inputs(T, d, dtype, 3 * T + d)
+    out = laep.moe_layer_norm(x, gamma, beta, residual=res)
+    _check_norm(x, res, gamma, beta, dtype, out)
+    got = laep.moe_layer_norm_bwd(dy, out[1], gamma, out[2], out[3], dres=res)
+    _check_norm_bwd(out[1], dy, gamma, out[2], out[3], res, dtype, got)
+    # x and the residual's gradient written in place, by rows beside each other
+    a, b = x.clone(), dy.clone()
+    assert torch.equal(laep.moe_layer_norm(a, gamma, beta, residual=res, sum_out=a)[0], out[0])
+    assert torch.equal(a, out[1])
+    again = laep.moe_layer_norm_bwd(b, out[1], gamma, out[2], out[3], dres=res, dx=b)
+    for p, q in zip(again, got):
+        assert torch.equal(p, q)
+    _check_norm(x, None, gamma, None, dtype, laep.moe_layer_norm(x, gamma))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [264, 2048, 8200, 16384])
 def test_layer_norm_in_place(d, dtype):
