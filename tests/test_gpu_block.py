@@ -260,6 +260,23 @@ def test_balance_loss(T, E, k, S, dead):
     _check_balance_bwd(logits, alive, off, got[3], acc, -3.0, base.astype(np.float64))
 
 
+# far more sequences than tokens, nearly all empty, and tokens of none before, between
+# and after them
+@pytest.mark.parametrize("T,E,S", [(1, 8, 300), (4, 64, 2000), (7, 45, 3), (300, 64, 5000)])
+@pytest.mark.parametrize("gaps", [False, True])
+def test_balance_empty_sequences(T, E, S, gaps):
+    case(f"balance loss T={T} E={E} sequences={S} gaps={gaps}")
+    logits, idx, _, off = _balance_inputs(T, E, 2, S, 0, T + S)
+    if gaps:   # the first and the last token outside
+        off = np.clip(off, min(1, T - 1), max(T - 1, 1)).astype(np.int32)
+    lt, it, ot = dev(logits, F32), dev(idx, torch.int32), dev(off, torch.int32)
+    got = laep.moe_balance_loss(lt, it, coef=0.02, seq_offsets=ot)
+    _check_balance(logits, idx, None, off, 0.02, got)
+    dl = laep.moe_balance_loss_bwd(lt, got[3], seq_offsets=ot)
+    _check_balance_bwd(logits, None, off, got[3], dl)
+    assert not dl[:off[0]].any() and not dl[off[-1]:].any()
+
+
 @pytest.mark.parametrize("E", [3, 45, 64, 253])
 def test_balance_gradient_in_place(E):
     T, k = 1500, 1
