@@ -17,7 +17,11 @@
 //
 // A token's row belongs to G lanes of four experts each (G the power of two from
 // E / 4 up), so a wave reads 64 / G rows at a time in whole lines and a softmax takes
-// log2 G lane moves for its maximum and its sum.
+// log2 G lane moves for its maximum and its sum.  The vector units are as busy as HBM
+// where G lanes hold far fewer than 4 G experts (60 instructions a row and wave), so row
+// addresses are a scalar base and the lane's own place, and rows inside a segment are not
+// checked: 83022 tokens of 77 experts in 25 sequences, forward and backward, 30.2 us for
+// 36.6, 32768 of 45 in 24 18.1 for 20.7.
 #include <type_traits>
 
 #include "common.hpp"
@@ -33,15 +37,15 @@ constexpr int kBalMaxE = 256;
 constexpr int kBalAhead = 4;         // rows of a lane group in flight
 constexpr int kBalIds = 4;           // slots of a thread loaded ahead
 constexpr int kBalMaxChunks = 1024;
-constexpr int kSumThreads = 1024;    // second pass: 16 lanes of four experts, 64 slots side by side
-constexpr int kSumCols = 64, kSumRows = kSumThreads / (kSumCols / 4);
+constexpr int kSumThreads = 1024, kSumCols = 64, kSumColsFew = 16;   // second pass
+constexpr int kLastParts = 32;       // parts of the loss that the last workgroup adds
 
 struct BalWs {          // carved from the workspace
   int* live;            // non-empty sequences
   int* done;            // workgroups of the second pass that have their part of the loss
   float* part_p;        // [slots, Ep], Ep: E rounded up to 4
   int* part_n;          // [slots, Ep]
-  float* part_loss;     // [n_seq, column blocks]
+  float* part_loss;     // [n_seq, column blocks], or kLastParts
 };
 
 __host__ __device__ inline int bal_ep(int E) { return (E + 3) & ~3; }
@@ -50,7 +54,7 @@ inline int bal_lanes(int E) {
   while (4 * g < E) g *= 2;
   return g;
 }
-inline int bal_blocks(int E) { return (E + kSumCols - 1) / kSumCols; }
+inline int bal_blocks(int E, int cols) { return (E + cols - 1) / cols; }
 
 // Tokens per chunk: two passes of the workgroup's rows at least, and 32; fewer where that
 // would put many sequences into a chunk, which takes them one after the other (about
@@ -87,7 +91,8 @@ inline size_t bal_carve(void* ws, int T, int E, int S, BalWs& w) {
   w.done = w.live + 1;
   w.part_p = reinterpret_cast<float*>(take(cells * 4));
   w.part_n = reinterpret_cast<int*>(take(cells * 4));
-  w.part_loss = reinterpret_cast<float*>(take((size_t)S * bal_blocks(E) * 4));
+  const size_t parts = (size_t)S * bal_blocks(E, kSumCols);
+  w.part_loss = reinterpret_cast<float*>(take((parts > kLastParts ? parts : kLastParts) * 4));
   return at;
 }
 
@@ -107,7 +112,7 @@ __device__ __forceinline__ int first_seq(const int32_t* __restrict__ off, int n_
   while (len > 0) {
     const int piece = (len + kWave - 1) / kWave;
     const bool past = lane * piece < len && off[lo + min((lane + 1) * piece, len)] <= t;
-    const int n = min(__popcll(__ballot(past)) * piece, len);   // ended by t
+    const int n = min((int)__popcll(__ballot(past)) * piece, len);   // ended by t
     lo += n;
     len = piece == 1 ? 0 : min(piece - 1, len - n);
   }
@@ -122,41 +127,56 @@ __device__ __forceinline__ int past_empty(const int32_t* __restrict__ off, int n
   return max(s, first_seq(off, n_seq, t) - 1);
 }
 
-// Four experts of a row, 4 l .. 4 l + 3, of a lane whose first is one.  Streaming loads:
-// what the caches hold is still found there, and the rest does not push out what other
-// calls wrote (131072 x 256, first pass: 43 -> 28 us).  VEC: E is a multiple of four and
-// rows are 16-byte aligned; else a lane's four are loaded together all the same, 4-byte
-// aligned, the last lane's from the row's last four and shifted (131072 tokens trained,
-// four single loads / one: 45 experts 39 / 30 us, 131 100 / 77, 250 161 / 97).
-typedef f32x4_t f32x4_a4_t __attribute__((aligned(4)));
-template <bool VEC>
-__device__ __forceinline__ void load4(const float* __restrict__ row, int e0, int E, float v[4]) {
-  if (VEC || E >= 4) {
-    const int at = VEC ? e0 : min(e0, E - 4), shift = e0 - at;
-    f32x4_t r;
-    if constexpr (VEC) r = ld_stream(reinterpret_cast<const f32x4_t*>(row + at));
-    else r = __builtin_nontemporal_load(reinterpret_cast<const f32x4_a4_t*>(row + at));
-    if (!VEC && (shift & 1)) r = f32x4_t{r[1], r[2], r[3], r[3]};
-    if (!VEC && (shift & 2)) r = f32x4_t{r[2], r[3], r[3], r[3]};
+// The four experts of a lane: e .. e + 3 of a row, whose own (alive) ones are ok.  The
+// last lane of a row takes the row's last four where E is no multiple of four, those of
+// the lane before being not its own; lanes past the row own none.  With fewer experts
+// than four, the one lane's first E.
+struct Quad {
+  int e;
+  bool ok[4];
+  bool whole;   // all four of the row, whatever is alive
+};
+__device__ __forceinline__ Quad quad_of(int lane, int E, const uint8_t* __restrict__ alive) {
+  Quad q;
+  const int e0 = 4 * lane;
+  q.e = max(0, min(e0, E - 4));
+  uint8_t a[4];   // (loaded together, whatever is masked)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = r[i];
-  } else {
+  for (int i = 0; i < 4; ++i) a[i] = alive == nullptr ? 1 : alive[min(q.e + i, E - 1)];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = e0 + i < E ? row[e0 + i] : 0.0f;
-  }
+  for (int i = 0; i < 4; ++i) q.ok[i] = q.e + i >= e0 && q.e + i < E && a[i] != 0;
+  q.whole = e0 + 4 <= E;
+  return q;
+}
+// expert i of a lane is its own, alive or not
+__device__ __forceinline__ bool own(const Quad& q, int lane, int i, int E) {
+  return q.e + i >= 4 * lane && q.e + i < E;
 }
 
-// Softmax of a row over its G lanes, logits to probabilities.  exp(l - m) is taken as
-// 2^(l log2 e - m log2 e), the rounding of m log2 e being common to the row: one fma
-// and the hardware's exp2 (an ulp) instead of a library call of a dozen instructions.
-// A row without a logit above -inf gets zeros.
+// Streaming loads of a lane's four: what the caches hold is still found there, and the
+// rest does not push out what other calls wrote (131072 x 256, first pass: 43 -> 28 us).
+// VEC: E is a multiple of four and rows are 16-byte aligned; else the four are loaded
+// together all the same, 4-byte aligned (131072 tokens trained, four single loads / one:
+// 45 experts 39 / 30 us, 131 100 / 77, 250 161 / 97).
+typedef f32x4_t f32x4_a4_t __attribute__((aligned(4)));
+template <bool VEC>
+__device__ __forceinline__ f32x4_t load4(const float* __restrict__ p, int E) {
+  if constexpr (VEC) return ld_stream(reinterpret_cast<const f32x4_t*>(p));
+  if (E >= 4) return __builtin_nontemporal_load(reinterpret_cast<const f32x4_a4_t*>(p));
+  return f32x4_t{p[0], E > 1 ? p[1] : 0.0f, E > 2 ? p[2] : 0.0f, 0.0f};
+}
+
+// exp(l - m) of a row over its G lanes, m its maximum; returns 1 / their sum.  exp(l - m)
+// is taken as 2^(l log2 e - m log2 e), the rounding of m log2 e being common to the row:
+// one fma and the hardware's exp2 (an ulp) instead of a library call of a dozen
+// instructions.  A row without a logit above -inf gets zeros.
 template <int G>
-__device__ __forceinline__ void softmax4(const bool ok[4], float v[4]) {
+__device__ __forceinline__ float exps4(const bool ok[4], const f32x4_t& l, float v[4]) {
   constexpr float kLog2e = 1.44269504f;
   float m = -INFINITY;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    v[i] = ok[i] ? v[i] : -INFINITY;
+    v[i] = ok[i] ? l[i] : -INFINITY;
     m = fmaxf(m, v[i]);
   }
   m = lanes_max<G>(m);
@@ -168,18 +188,31 @@ __device__ __forceinline__ void softmax4(const bool ok[4], float v[4]) {
     z += v[i];
   }
   z = lanes_sum<G>(z);
-  const float inv = z == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(z);   // else z >= 1 (or a NaN)
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] *= inv;
+  return z == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(z);   // else z >= 1 (or a NaN)
 }
 
-__device__ __forceinline__ void load_alive(const uint8_t* __restrict__ alive, int E, int e0,
-                                           bool ok[4]) {
-  uint8_t a[4];   // (loaded together, whatever is masked)
+// f(row, the lane's four logits, row < n) for the rows of a segment of n, kBalAhead loads
+// in flight.  The addresses are a uniform base and the lane's place; rows past the segment
+// load its last row's bytes.
+template <bool VEC, int ROWS, typename F>
+__device__ __forceinline__ void walk_rows(const float* seg, int n, int E, int first, int e, F f) {
+  const unsigned at = first * E + e;
+  int r = 0;
+  for (; r + ROWS * kBalAhead <= n; r += ROWS * kBalAhead) {  // (uniform)
+    f32x4_t l[kBalAhead];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) a[i] = alive == nullptr ? 1 : alive[min(e0 + i, E - 1)];
+    for (int u = 0; u < kBalAhead; ++u) l[u] = load4<VEC>(seg + (size_t)(r + u * ROWS) * E + at, E);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) ok[i] = e0 + i < E && a[i] != 0;
+    for (int u = 0; u < kBalAhead; ++u) f(r + u * ROWS + first, l[u], true);
+  }
+  if (r >= n) return;
+  f32x4_t l[kBalAhead];
+#pragma unroll
+  for (int u = 0; u < kBalAhead; ++u)
+    l[u] = load4<VEC>(seg + (size_t)min(r + u * ROWS + first, n - 1) * E + e, E);
+#pragma unroll
+  for (int u = 0; u < kBalAhead; ++u)
+    if (r + u * ROWS < n) f(r + u * ROWS + first, l[u], r + u * ROWS + first < n);
 }
 
 struct BalOut {
@@ -220,7 +253,7 @@ __global__ __launch_bounds__(kBalThreads) void balance_chunk_kernel(
   __shared__ int s_live;
   __shared__ float s_loss[kBalWaves];
   const int tid = threadIdx.x, wave = tid / kWave, lane = tid & (kWave - 1);
-  const int e0 = 4 * (lane % G), ep = bal_ep(E);
+  const int ep = bal_ep(E);
   int n_alive = E;
   if (ONE || blockIdx.x == gridDim.x - 1) {  // needed once: by the last workgroup, or the one
     if (tid == 0) s_live = 0;
@@ -242,8 +275,7 @@ __global__ __launch_bounds__(kBalThreads) void balance_chunk_kernel(
       return;
     }
   }
-  bool ok[4];
-  load_alive(alive, E, e0, ok);
+  const Quad q = quad_of(lane % G, E, alive);
   const int t0 = blockIdx.x * chunk, t1 = T - t0 < chunk ? T : t0 + chunk;
   float loss = 0.0f;
   int done = t0;
@@ -268,23 +300,13 @@ __global__ __launch_bounds__(kBalThreads) void balance_chunk_kernel(
       ids[u] = i0 + u * kBalThreads < i1 ? topk_idx[i0 + u * kBalThreads] : -1;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     const int first = wave * RPW + lane / G;
-    for (int r = 0; r < b - a; r += ROWS * kBalAhead) {  // (uniform: every lane moves along)
-      float v[kBalAhead][4];
+    const auto add = [&](int, const f32x4_t& l, bool on) {
+      float v[4];
+      const float inv = exps4<G>(q.ok, l, v);
 #pragma unroll
-      for (int u = 0; u < kBalAhead; ++u) {
-        const int row = r + u * ROWS + first;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[u][i] = -INFINITY;
-        if (row < b - a && e0 < E)
-          load4<VEC>(logits + (size_t)(a + row) * E, e0, E, v[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < kBalAhead; ++u) {
-        softmax4<G>(ok, v[u]);   // rows past the sequence: all -inf, zeros
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] += v[u][i];
-      }
-    }
+      for (int i = 0; i < 4; ++i) sum[i] = on ? fmaf(v[i], inv, sum[i]) : sum[i];
+    };
+    walk_rows<VEC, ROWS>(logits + (size_t)a * E, b - a, E, first, q.e, add);
 #pragma unroll
     for (int u = 0; u < kBalIds; ++u)
       if (ids[u] >= 0 && ids[u] < E) atomicAdd(&s_n[ids[u]], 1);
@@ -296,8 +318,11 @@ __global__ __launch_bounds__(kBalThreads) void balance_chunk_kernel(
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int d = G; d < kWave; d *= 2) sum[i] += __shfl_xor(sum[i], d, kWave);
-    if (lane < G)
-      *reinterpret_cast<f32x4_t*>(&s_p[wave][e0]) = f32x4_t{sum[0], sum[1], sum[2], sum[3]};
+    if (lane < G) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (own(q, lane, i, E)) s_p[wave][q.e + i] = sum[i];
+    }
     __syncthreads();
     if (tid < E) {
       float p = 0.0f;
@@ -326,43 +351,60 @@ __global__ __launch_bounds__(kBalThreads) void balance_chunk_kernel(
   }
 }
 
-// Second pass: 64 experts of one sequence per workgroup, its slots 64 side by side and
-// those in order.  The loss: alone, the workgroup has it; up to kLastParts workgroups the
-// one that finishes last adds their parts, in their order (its counter was cleared by the
-// first pass); with more, whose release of the counter costs more than it saves, a third
-// kernel does.  Whole call, third kernel / last workgroup, 20000 tokens: 8 workgroups 12.9 /
-// 11.2 us, 32 12.9 / 11.4, 64 13.0 / 12.5, 256 15.3 / 19.7.
-constexpr int kLastParts = 32;
+// Second pass: COLS experts of one sequence per workgroup, its slots side by side, then
+// those of a wave and of the waves in order.  16 experts a workgroup instead of 64 where
+// that makes no more than kLastParts of them, for few sequences have many slots each:
+// 28300 tokens of 256 experts in one sequence, forward and backward, 28.7 us for 30.5,
+// 20000 of 128 17.8 for 18.7.
+// The loss: alone, the workgroup has it; up to kLastParts workgroups the one that finishes
+// last adds their parts, in their order (its counter was cleared by the first pass); with
+// more, whose release of the counter costs more than it saves, a third kernel does.  Whole
+// call, third kernel / last workgroup, 20000 tokens: 8 workgroups 12.9 / 11.2 us, 32 12.9 /
+// 11.4, 64 13.0 / 12.5, 256 15.3 / 19.7.
+template <int COLS>
 __global__ __launch_bounds__(kSumThreads) void balance_sum_kernel(
     const uint8_t* __restrict__ alive, const int32_t* __restrict__ off, int T, int E, int k,
     int n_seq, int chunk, BalWs w, BalOut o) {
-  __shared__ __attribute__((aligned(16))) float s_p[kSumRows][kSumCols];
-  __shared__ __attribute__((aligned(16))) int s_n[kSumRows][kSumCols];
+  constexpr int LC = COLS / 4, ROWS = kSumThreads / LC, WAVES = kSumThreads / kWave;
+  __shared__ __attribute__((aligned(16))) float s_p[WAVES][COLS];
+  __shared__ __attribute__((aligned(16))) int s_n[WAVES][COLS];
   typedef int i32x4_t __attribute__((ext_vector_type(4)));
-  const int tid = threadIdx.x, col = (tid % (kSumCols / 4)) * 4, row = tid / (kSumCols / 4);
-  const int s = blockIdx.x, e = blockIdx.y * kSumCols + col, ep = bal_ep(E);
+  const int tid = threadIdx.x, col = (tid % LC) * 4, row = tid / LC;
+  const int s = blockIdx.x, e = blockIdx.y * COLS + col, ep = bal_ep(E);
   const int n_alive = alive == nullptr ? E : __syncthreads_count(tid < E && alive[tid] != 0);
   int a, b;
   seq_range(off, s, T, a, b);
   f32x4_t p = {0.f, 0.f, 0.f, 0.f};
   i32x4_t n = {0, 0, 0, 0};
-  if (b > a && e < E)
-    for (int c = a / chunk + row; c <= (b - 1) / chunk; c += kSumRows) {
+  const int c0 = a / chunk, c1 = b > a ? (b - 1) / chunk : -1;
+  if (c0 + tid / kWave * (kWave / LC) <= c1) {   // the wave has slots
+    for (int c = c0 + row; c <= c1 && e < E; c += ROWS) {
       const size_t at = ((size_t)c + s) * ep + e;
       p += *reinterpret_cast<const f32x4_t*>(w.part_p + at);
       n += *reinterpret_cast<const i32x4_t*>(w.part_n + at);
     }
-  *reinterpret_cast<f32x4_t*>(&s_p[row][col]) = p;
-  *reinterpret_cast<i32x4_t*>(&s_n[row][col]) = n;
+#pragma unroll
+    for (int d = LC; d < kWave; d *= 2) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[i] += __shfl_xor(p[i], d, kWave);
+        n[i] += __shfl_xor(n[i], d, kWave);
+      }
+    }
+  }
+  if (tid % kWave < LC) {
+    *reinterpret_cast<f32x4_t*>(&s_p[tid / kWave][col]) = p;
+    *reinterpret_cast<i32x4_t*>(&s_n[tid / kWave][col]) = n;
+  }
   __syncthreads();
-  if (tid >= kSumCols) return;   // one wave from here, an expert each
-  const int my = blockIdx.y * kSumCols + tid;
+  if (tid >= kWave) return;   // one wave from here, an expert a lane
+  const int my = blockIdx.y * COLS + tid;
   float part = 0.0f;
-  if (my < E) {
+  if (tid < COLS && my < E) {
     float ps = 0.0f;
     int ns = 0;
-#pragma unroll 8
-    for (int i = 0; i < kSumRows; ++i) {
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
       ps += s_p[i][tid];
       ns += s_n[i][tid];
     }
@@ -414,26 +456,21 @@ __global__ __launch_bounds__(kBalThreads) void balance_bwd_kernel(
     int range, float* dlogits, int accumulate) {
   constexpr int RPW = kWave / G, ROWS = kBalWaves * RPW;
   const int tid = threadIdx.x, wave = tid / kWave, lane = tid & (kWave - 1);
-  const int e0 = 4 * (lane % G), first = wave * RPW + lane / G;
-  bool ok[4];
-  load_alive(alive, E, e0, ok);
+  const int l0 = lane % G, first = wave * RPW + lane / G;
+  const Quad q = quad_of(l0, E, alive);
   const float scale = dloss ? *dloss : 1.0f;
   const int t0 = blockIdx.x * range, t1 = T - t0 < range ? T : t0 + range;
   auto put = [&](int t, const float v[4]) {
-    float* const d = dlogits + (size_t)t * E + e0;
-    if constexpr (VEC) {
-      if (e0 >= E) return;
+    float* const d = dlogits + (size_t)t * E + q.e;
+    if (q.whole) {
+      using V = std::conditional_t<VEC, f32x4_t, f32x4_a4_t>;
       f32x4_t r = {v[0], v[1], v[2], v[3]};
-      if (accumulate) r += *reinterpret_cast<f32x4_t*>(d);
-      *reinterpret_cast<f32x4_t*>(d) = r;
-    } else if (e0 + 4 <= E) {
-      f32x4_t r = {v[0], v[1], v[2], v[3]};
-      if (accumulate) r += *reinterpret_cast<f32x4_a4_t*>(d);
-      *reinterpret_cast<f32x4_a4_t*>(d) = r;
-    } else {
+      if (accumulate) r += *reinterpret_cast<V*>(d);
+      *reinterpret_cast<V*>(d) = r;
+    } else if (!VEC) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (e0 + i < E) d[i] = accumulate ? d[i] + v[i] : v[i];
+        if (own(q, l0, i, E)) d[i] = accumulate ? d[i] + v[i] : v[i];
     }
   };
   auto zeros = [&](int from, int to) {
@@ -456,30 +493,18 @@ __global__ __launch_bounds__(kBalThreads) void balance_bwd_kernel(
     done = b;
     float c[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = ok[i] ? grad_coef[(size_t)s * E + e0 + i] : 0.0f;
-    for (int r = 0; r < b - a; r += ROWS * kBalAhead) {
-      float v[kBalAhead][4];
+    for (int i = 0; i < 4; ++i) c[i] = q.ok[i] ? grad_coef[(size_t)s * E + q.e + i] : 0.0f;
+    const auto grad = [&](int row, const f32x4_t& l, bool on) {
+      float v[4], dot = 0.0f;
+      const float inv = exps4<G>(q.ok, l, v);
 #pragma unroll
-      for (int u = 0; u < kBalAhead; ++u) {
-        const int row = r + u * ROWS + first;
+      for (int i = 0; i < 4; ++i) dot += v[i] * c[i];
+      dot = lanes_sum<G>(dot) * inv;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[u][i] = -INFINITY;
-        if (row < b - a && e0 < E)
-          load4<VEC>(logits + (size_t)(a + row) * E, e0, E, v[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < kBalAhead; ++u) {
-        softmax4<G>(ok, v[u]);
-        float dot = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dot += v[u][i] * c[i];
-        dot = lanes_sum<G>(dot);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[u][i] = ok[i] ? scale * v[u][i] * (c[i] - dot) : 0.0f;
-        const int row = r + u * ROWS + first;
-        if (row < b - a) put(a + row, v[u]);
-      }
-    }
+      for (int i = 0; i < 4; ++i) v[i] = q.ok[i] ? scale * inv * v[i] * (c[i] - dot) : 0.0f;
+      if (on) put(a + row, v);
+    };
+    walk_rows<VEC, ROWS>(logits + (size_t)a * E, b - a, E, first, q.e, grad);
   }
   zeros(done, t1);
 }
@@ -525,14 +550,17 @@ hipError_t launch_balance(const float* logits, const int32_t* topk_idx, const ui
   bal_shape(E, [&](auto g, auto vec) {
     constexpr int G = decltype(g)::value;
     constexpr bool VEC = decltype(vec)::value;
-    const auto kernel = one ? balance_chunk_kernel<G, VEC, true> : balance_chunk_kernel<G, VEC, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(one ? 1 : extra)), dim3(kBalThreads), 0, s, logits, topk_idx,
-                       alive, seq_offsets, T, E, k, n_seq, chunk, w, o);
+    const auto kernel = one ? balance_chunk_kernel<G, VEC, true>
+                            : balance_chunk_kernel<G, VEC, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(one ? 1 : extra)), dim3(kBalThreads), 0, s,
+                       logits, topk_idx, alive, seq_offsets, T, E, k, n_seq, chunk, w, o);
   });
   if (one) return hipGetLastError();
-  const int blocks = bal_blocks(E);
-  hipLaunchKernelGGL(balance_sum_kernel, dim3((unsigned)n_seq, (unsigned)blocks),
-                     dim3(kSumThreads), 0, s, alive, seq_offsets, T, E, k, n_seq, chunk, w, o);
+  const bool few = n_seq * bal_blocks(E, kSumColsFew) <= kLastParts;
+  const int blocks = bal_blocks(E, few ? kSumColsFew : kSumCols);
+  hipLaunchKernelGGL(few ? balance_sum_kernel<kSumColsFew> : balance_sum_kernel<kSumCols>,
+                     dim3((unsigned)n_seq, (unsigned)blocks), dim3(kSumThreads), 0, s, alive,
+                     seq_offsets, T, E, k, n_seq, chunk, w, o);
   if (n_seq * blocks > kLastParts)
     hipLaunchKernelGGL(balance_loss_kernel, dim3(1), dim3(kWave), 0, s, w.part_loss,
                        n_seq * blocks, loss);

@@ -103,8 +103,8 @@ __device__ __forceinline__ float row_sum(float v) {
 template <typename T, int NL, int VPL, bool RES>
 __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_kernel(
     const T* x, const T* residual, const float* __restrict__ gamma,
-    const float* __restrict__ beta, unsigned n_rows, int d, float eps, T* sum_out, T* __restrict__ y,
-    float* __restrict__ mean, float* __restrict__ rstd) {
+    const float* __restrict__ beta, unsigned n_rows, int d, float eps, T* sum_out,
+    T* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd) {
   using S = NormShape<NL, kFwdThreads>;
   constexpr int N = Vec<T>::N;
   __shared__ float s_red[2][S::NT / kWave][2];
@@ -391,8 +391,9 @@ __global__ __launch_bounds__(256) void norm_bwd_reduce_kernel(const float* __res
       f32x4_t v[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u)
-        v[u] = i + 16 * u < n_part ? *reinterpret_cast<const f32x4_t*>(p + (size_t)(i + 16 * u) * 2 * d)
-                                   : f32x4_t{0.f, 0.f, 0.f, 0.f};
+        v[u] = i + 16 * u < n_part
+                   ? *reinterpret_cast<const f32x4_t*>(p + (size_t)(i + 16 * u) * 2 * d)
+                   : f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < 8; ++u) t += v[u];
     }
