@@ -78,7 +78,10 @@ __device__ __forceinline__ void load_f32(const float* p, float v[N]) {
 // use: with a branch round the loads the compiler cannot tell which are pending where the
 // paths join, and waits for the stores as well (8192 x 5120 69 us for 57, 3000 x 10240 58
 // for 49).
-// Forward with a residual: workgroups for 20 waves a CU, each row's loads issued after
+// The waves' parts of a row's sums are added by lanes of each wave, a part a lane: every
+// lane reading all of them took 93 registers for 47 at 1024 lanes of bf16, and a CU's
+// second workgroup (12000 x 7168 bf16 without a residual 89 us for 66).
+// Forward with a residual: workgroups for about 19 waves a CU, each row's loads issued after
 // the last one's stores: 181 us at 32768 x 4096 bf16 (5.9 TB/s of 6.2 that a copy
 // reaches), 24 us at 8192 x 2048; loading the next row ahead 202 and 27, a workgroup for
 // every row 205 and 26.  Without one a row has half the loads, and the next row's go
@@ -92,6 +95,8 @@ template <int NL, int MOST> struct NormShape {
   static constexpr int ROWS = NL < MOST ? MOST / NL : 1;     // rows at a time
   static constexpr int NT = ROWS * NL;
   static constexpr int WAVES = NL > kWave ? NL / kWave : 1;  // waves of a row
+  // lanes that add the waves' parts: a power of two
+  static constexpr int PARTS = WAVES > 8 ? 16 : WAVES > 4 ? 8 : WAVES > 2 ? 4 : WAVES;
 };
 
 // sum over the row's lanes inside a wave
@@ -112,7 +117,6 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
   const int l = threadIdx.x % NL, sub = threadIdx.x / NL;
   const int wave = threadIdx.x / kWave, wave0 = wave - wave % S::WAVES;
   float g[VPL][N], b[VPL][N];
-  int cols = 0;               // columns of this wave's part of a row
 #pragma unroll
   for (int u = 0; u < VPL; ++u) {
     const int v = l + u * NL;
@@ -122,9 +126,18 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
       load_f32<N>(gamma + (size_t)v * N, g[u]);
       if (beta) load_f32<N>(beta + (size_t)v * N, b[u]);
     }
-    if (NL > kWave) cols += N * min(kWave, max(0, nvec - u * NL - (wave % S::WAVES) * kWave));
   }
-  if (NL <= kWave) cols = d;
+  // columns of a row that its wave w holds
+  auto cols_of = [&](int w) {
+    if (NL <= kWave) return d;
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < VPL; ++u) n += N * min(kWave, max(0, nvec - u * NL - w * kWave));
+    return n;
+  };
+  const int cols = cols_of(wave % S::WAVES);
+  const int w = threadIdx.x % S::PARTS;    // the wave whose part this lane adds
+  const float cols_w = w < S::WAVES ? (float)cols_of(w) : 0.0f;
   Vec<T> xv[VPL], rv[VPL];
   auto load = [&](unsigned row) {
 #pragma unroll
@@ -180,22 +193,10 @@ __global__ __launch_bounds__((NormShape<NL, kFwdThreads>::NT)) void norm_fwd_ker
         s_red[it][wave][1] = sq;
       }
       __syncthreads();
-      float tot = 0.0f;
-      int n[S::WAVES];
-#pragma unroll
-      for (int w = 0; w < S::WAVES; ++w) {
-        n[w] = 0;
-#pragma unroll
-        for (int u = 0; u < VPL; ++u) n[w] += N * min(kWave, max(0, nvec - u * NL - w * kWave));
-        tot += s_red[it][wave0 + w][0] * (float)n[w];
-      }
-      mu = tot / (float)d;
-      sq = 0.0f;
-#pragma unroll
-      for (int w = 0; w < S::WAVES; ++w) {
-        const float off = s_red[it][wave0 + w][0] - mu;
-        sq += s_red[it][wave0 + w][1] + (float)n[w] * off * off;
-      }
+      const float* const part = s_red[it][wave0 + min(w, S::WAVES - 1)];
+      const float mu_w = part[0], sq_w = w < S::WAVES ? part[1] : 0.0f;
+      mu = lanes_sum<S::PARTS>(mu_w * cols_w) / (float)d;
+      sq = lanes_sum<S::PARTS>(sq_w + cols_w * (mu_w - mu) * (mu_w - mu));
     }
     const float rs = 1.0f / sqrtf(sq / (float)d + eps);
     if (row < n_rows) {
@@ -308,12 +309,10 @@ __global__ __launch_bounds__((NormShape<NL, kBwdThreads>::NT)) void norm_bwd_ker
         s_red[it][wave][1] = b;
       }
       __syncthreads();
-      a = b = 0.0f;
-#pragma unroll
-      for (int w = 0; w < S::WAVES; ++w) {
-        a += s_red[it][wave0 + w][0];
-        b += s_red[it][wave0 + w][1];
-      }
+      const int w = threadIdx.x % S::PARTS;
+      const float* const part = s_red[it][wave0 + min(w, S::WAVES - 1)];
+      a = lanes_sum<S::PARTS>(w < S::WAVES ? part[0] : 0.0f);
+      b = lanes_sum<S::PARTS>(w < S::WAVES ? part[1] : 0.0f);
     }
     a /= (float)d;
     b /= (float)d;
@@ -547,11 +546,12 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_wide_kernel(
   }
 }
 
-// Workgroups of a call.  Forward: waves a CU with a residual and without one: with it 24
-// take 188 us for 181 at 32768 x 4096 bf16, 86 for 81 at 30000 x 1000 float32, though 39
-// for 42 at 40000 x 640 bf16; without, 16 take 34 us for 28 at 24607 x 768 float32, 16 for
-// 15 at 8192 x 2048 bf16, and 32 take 64 for 56 at 29392 x 2240.
-constexpr int kCus = 256, kFwdWaves = 20, kFwdWavesAlone = 24, kBwdGroups = 256;
+// Workgroups of a call.  Forward: as many a CU as come nearest to these waves, with a
+// residual and without one: with it 24 take 188 us for 181 at 32768 x 4096 bf16, 86 for 80
+// at 30000 x 1000 float32, though 38 for 42 at 40000 x 640 bf16; without, 16 take 34 us
+// for 28 at 24607 x 768 float32, 16 for 15 at 8192 x 2048 bf16, and 32 take 62 for 54 at
+// 29392 x 2240; rounded down, 16-wave rows keep 16: 84 us for 66 at 12000 x 7168.
+constexpr int kCus = 256, kFwdWaves = 19, kFwdWavesAlone = 24, kBwdGroups = 256;
 
 // f(lanes per row, vectors per lane) for rows of d columns; false past 16384.
 template <typename T, typename F>
@@ -607,7 +607,8 @@ hipError_t norm_fwd_t(const T* x, const T* residual, const float* gamma, const f
     using S = NormShape<NL, kFwdThreads>;
     const int need = (n - 1) / S::ROWS + 1;
     const auto run = [&](auto kernel, int waves) {
-      const int per = waves / (S::NT / kWave), most = kCus * (per > 1 ? per : 1);
+      constexpr int W = S::NT / kWave;
+      const int per = (waves + W / 2) / W, most = kCus * (per > 1 ? per : 1);
       hipLaunchKernelGGL(kernel, dim3((unsigned)(need < most ? need : most)), dim3(S::NT), 0, s, x,
                          residual, gamma, beta, n, d, eps, sum_out, y, mean, rstd);
     };
