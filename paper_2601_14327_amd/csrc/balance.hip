@@ -167,9 +167,11 @@ __device__ __forceinline__ f32x4_t load4(const float* __restrict__ p, int E) {
 }
 
 // exp(l - m) of a row over its G lanes, m its maximum; returns 1 / their sum.  exp(l - m)
-// is taken as 2^(l log2 e - m log2 e), the rounding of m log2 e being common to the row:
-// one fma and the hardware's exp2 (an ulp) instead of a library call of a dozen
-// instructions.  A row without a logit above -inf gets zeros.
+// is taken as 2^((l - m) log2 e): one subtraction, one product and the hardware's exp2 (an
+// ulp) instead of a library call of a dozen instructions.  The maximum is subtracted first:
+// it then gives exactly 1 whatever its size, rows of one finite mask value are uniform, and
+// no finite logit overflows (a difference past the range is -inf, hence 0).  A row without a
+// logit above -inf gets zeros.
 template <int G>
 __device__ __forceinline__ float exps4(const bool ok[4], const f32x4_t& l, float v[4]) {
   constexpr float kLog2e = 1.44269504f;
@@ -180,11 +182,11 @@ __device__ __forceinline__ float exps4(const bool ok[4], const f32x4_t& l, float
     m = fmaxf(m, v[i]);
   }
   m = lanes_max<G>(m);
-  const float base = m == -INFINITY ? 0.0f : m * kLog2e;
+  const float base = m == -INFINITY ? 0.0f : m;
   float z = 0.0f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    v[i] = __builtin_amdgcn_exp2f(fmaf(v[i], kLog2e, -base));
+    v[i] = __builtin_amdgcn_exp2f((v[i] - base) * kLog2e);
     z += v[i];
   }
   z = lanes_sum<G>(z);
