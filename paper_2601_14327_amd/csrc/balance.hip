@@ -477,8 +477,8 @@ __global__ __launch_bounds__(kBalThreads) void balance_bwd_kernel(
   };
   auto zeros = [&](int from, int to) {
     const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (!accumulate)
-      for (int t = from + first; t < to; t += ROWS) put(t, z);
+    if (!accumulate)   // (T may come near 2^31: counted from the range's start)
+      for (int r = first; r < to - from; r += ROWS) put(from + r, z);
   };
   int done = t0;
   for (int s = first_seq(off, n_seq, t0); s < n_seq; ++s) {
