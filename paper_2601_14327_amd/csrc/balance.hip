@@ -119,8 +119,9 @@ __device__ __forceinline__ int first_seq(const int32_t* __restrict__ off, int n_
   return lo;
 }
 
-// The sequence to go on with after an empty one, tokens up to t being done: the next that
-// ends past t, for the loop's own step to reach (forwards whatever the offsets hold).
+// The sequence to go on with after one that is empty at token t: the next that ends past
+// t, for the loop's own step to reach (forwards whatever the offsets hold).  t is the
+// empty one's own place, not the last token done: tokens of no sequence may lie between.
 // 2000 sequences of 4 tokens in all: 21 us, one after the other 111.
 __device__ __forceinline__ int past_empty(const int32_t* __restrict__ off, int n_seq, int s,
                                           int t) {
@@ -280,7 +281,6 @@ __global__ __launch_bounds__(kBalThreads) void balance_chunk_kernel(
   const Quad q = quad_of(lane % G, E, alive);
   const int t0 = blockIdx.x * chunk, t1 = T - t0 < chunk ? T : t0 + chunk;
   float loss = 0.0f;
-  int done = t0;
   for (int s = ONE ? 0 : first_seq(off, n_seq, t0); s < n_seq; ++s) {
     int a, b;
     seq_range(off, s, T, a, b);
@@ -288,10 +288,9 @@ __global__ __launch_bounds__(kBalThreads) void balance_chunk_kernel(
     a = max(a, t0);
     b = min(b, t1);
     if (!ONE && a >= b) {  // (uniform)
-      s = past_empty(off, n_seq, s, done);
+      s = past_empty(off, n_seq, s, a);
       continue;
     }
-    done = b;
     for (int e = tid; e < E; e += kBalThreads) s_n[e] = 0;
     __syncthreads();
     // the slots' ids: the first ones travel under the logits
@@ -488,7 +487,7 @@ __global__ __launch_bounds__(kBalThreads) void balance_bwd_kernel(
     a = max(a, done);
     b = min(b, t1);
     if (a >= b) {  // (uniform)
-      s = past_empty(off, n_seq, s, done);
+      s = past_empty(off, n_seq, s, a);
       continue;
     }
     zeros(done, a);
