@@ -100,8 +100,9 @@ int moe_balance_loss(const float* logits, const int32_t* topk_idx,
  *   of the token's sequence s; dead experts and tokens of no sequence get 0.
  *
  *   dloss device [1] float32 or NULL (1); dlogits device [T, E] float32,
- *   overwritten or (accumulate = 1) added to; it may be logits' buffer only
- *   when not accumulating.  The other arguments as in moe_balance_loss.
+ *   overwritten or (accumulate = 1) added to; it may be logits' buffer when not
+ *   accumulating, and any other overlap with it is refused.  The other
+ *   arguments as in moe_balance_loss.
  */
 int moe_balance_loss_bwd(const float* logits, const float* grad_coef,
                          const uint8_t* alive, const int32_t* seq_offsets,

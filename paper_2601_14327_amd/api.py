@@ -656,7 +656,8 @@ def moe_balance_loss_bwd(logits: torch.Tensor, grad_coef: torch.Tensor, *, dloss
                          alive=None, seq_offsets=None, dlogits=None, accumulate: bool = False):
     """Gradient of the balance loss with respect to the logits, the counts held
     fixed; ``dloss`` is a float32 device tensor of one element (None: 1).
-    ``accumulate`` adds to the given dlogits."""
+    ``accumulate`` adds to the given dlogits, which must then not be the logits'
+    buffer (it may be otherwise)."""
     _dev(logits, "logits")
     T, E = logits.shape
     S = _sequences(seq_offsets)

@@ -35,6 +35,12 @@ int hip_status(hipError_t e, const char* where) {
   return ok();
 }
 
+// whether two buffers (NULL: none) share bytes
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x && y && (x < y ? y - x < a_bytes : x - y < b_bytes);
+}
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 #define REQUIRE(cond, code, ...) \
@@ -804,6 +810,11 @@ int moe_balance_loss_bwd(const float* logits, const float* grad_coef, const uint
           "moe_balance_loss_bwd: logits, grad_coef and dlogits must be non-null");
   REQUIRE(aligned16(logits) && aligned16(grad_coef) && aligned16(dlogits), LAEP_ERR_INVALID_ARG,
           "moe_balance_loss_bwd: logits, grad_coef and dlogits must be 16-byte aligned");
+  const size_t bytes = (size_t)T * E * sizeof(float);
+  REQUIRE((dlogits == logits && !accumulate) || !overlap(dlogits, bytes, logits, bytes),
+          LAEP_ERR_INVALID_ARG,
+          "moe_balance_loss_bwd: dlogits must not overlap logits (it may be their buffer when not "
+          "accumulating)");
   return hip_status(laep::launch_balance_bwd(logits, grad_coef, alive, seq_offsets, dloss, T, E,
                                              n_seq, dlogits, accumulate != 0, as_stream(stream)),
                     "moe_balance_loss_bwd");
