@@ -119,7 +119,8 @@ int moe_balance_loss_bwd(const float* logits, const float* grad_coef,
  *   Every alive expert carries a gradient, so the products are dense for
  *   renormalised gates too, and offsets and row_src are not needed.
  *
- *   logits device [T, E] float32 (moe_route's output, both kinds of gates);
+ *   logits device [T, E] float32 (moe_route's output, both kinds of gates),
+ *   which dlogits must not overlap;
  *   grad_coef, seq_offsets, n_seq, dloss as in moe_balance_loss_bwd; the other
  *   arguments, the workspace and T = 0 as in moe_route_bwd.
  */

@@ -682,7 +682,8 @@ def moe_route_bwd_balance(dgate: torch.Tensor, topk_idx: torch.Tensor, topk_gate
                           dlogits=None, dbias=None, ws=None, data: bool = True,
                           weights: bool = True):
     """moe_route_bwd with the balance loss's gradient (moe_balance_loss's
-    grad_coef) added to the gates' before the products.  Returns as moe_route_bwd."""
+    grad_coef) added to the gates' before the products.  ``dlogits`` must not be the
+    logits' buffer.  Returns as moe_route_bwd."""
     for t, n in ((dgate, "dgate"), (topk_idx, "topk_idx"), (topk_gate, "topk_gate"), (x, "x"),
                  (w_router, "w_router")):
         _dev(t, n)

@@ -416,6 +416,10 @@ int moe_route_bwd_balance(const float* dgate, const int32_t* topk_idx, const flo
                 aligned16(ws),
             LAEP_ERR_INVALID_ARG,
             "moe_route_bwd_balance: x, dx, logits, dlogits and ws must be 16-byte aligned");
+    const size_t bytes = (size_t)T * E * sizeof(float);
+    REQUIRE(!overlap(dlogits, bytes, logits, bytes), LAEP_ERR_INVALID_ARG,
+            "moe_route_bwd_balance: dlogits must not overlap logits (read after the gates' gradient "
+            "is written)");
     const size_t need = laep::route_bwd_ws_bytes(T, k, E, d_model);
     REQUIRE(ws_bytes >= need, LAEP_ERR_WORKSPACE,
             "moe_route_bwd_balance: workspace %zu < %zu bytes", ws_bytes, need);
