@@ -616,7 +616,7 @@ def _given_ws(ws, device, which, *sizes):
     if ws is None:
         return torch.empty(max(workspace_bytes(which, *sizes), 1), dtype=torch.uint8,
                            device=device)
-    return ws
+    return _dev(ws, "ws")
 
 
 def _scalar(t, name: str):
@@ -708,7 +708,7 @@ def moe_route_bwd_balance(dgate: torch.Tensor, topk_idx: torch.Tensor, topk_gate
         dw_router, dbias = None, None
     if want_dlogits or dlogits is not None:
         dlogits = _out(dlogits, "dlogits", (T, E), f32, dev)
-    ws = _workspace(ws, workspace_bytes(LAEP_CALL_ROUTE_BWD, T, k, E, d), dev)
+    ws = _given_ws(ws, dev, LAEP_CALL_ROUTE_BWD, T, k, E, d)
     check(lib().moe_route_bwd_balance(
         _ptr(dgate), _ptr(topk_idx), _ptr(topk_gate), _ptr(logits), _ptr(alive), _ptr(x),
         _ptr(w_router), _ptr(grad_coef), _ptr(seq_offsets), S, _ptr(dloss), _dtype_code(x), T, d,
@@ -790,12 +790,12 @@ def moe_grouped_ffn_bwd_gather_act8(dy_perm, x, row_src, k: int, act_q, act_scal
         dw_gate_up = torch.empty(w_gate_up.shape, dtype=torch.float32, device=dev)
     if dw_down is None:
         dw_down = torch.empty(w_down.shape, dtype=torch.float32, device=dev)
-    ws = _workspace(ws, workspace_bytes(LAEP_CALL_FFN_BWD, R, 1, E, d, f), dev)
+    ws = _given_ws(ws, dev, LAEP_CALL_FFN_BWD, R, 1, E, d, f)
     check(lib().moe_grouped_ffn_bwd_gather_act8(
         _ptr(dy_perm), _ptr(dout), _ptr(topk_gate), _ptr(x), _ptr(row_src), T, k, _ptr(act_q),
         _ptr(act_scale), _ptr(w_gate_up), _ptr(w_down), _ptr(offsets), _ptr(expert_map),
         _dtype_code(x), E, d, f, R, _ptr(dx_perm), _ptr(dw_gate_up), _ptr(dw_down),
-        int(accumulate), _ptr(ws), ws.numel(), _stream(dev)))
+        int(accumulate), _ptr(ws), ws.numel() * ws.element_size(), _stream(dev)))
     out = (dx_perm, dw_gate_up, dw_down)
     return out + (ws,) if return_ws else out
 
