@@ -684,25 +684,26 @@ def moe_route_bwd_balance(dgate: torch.Tensor, topk_idx: torch.Tensor, topk_gate
     """moe_route_bwd with the balance loss's gradient (moe_balance_loss's
     grad_coef) added to the gates' before the products.  ``dlogits`` must not be the
     logits' buffer.  Returns as moe_route_bwd."""
-    for t, n in ((dgate, "dgate"), (topk_idx, "topk_idx"), (topk_gate, "topk_gate"), (x, "x"),
-                 (w_router, "w_router")):
-        _dev(t, n)
     T, k = topk_idx.shape
     E, d = w_router.shape
     dev = x.device
     f32 = torch.float32
     S = _sequences(seq_offsets)
+    _want(dgate, "dgate", (T, k), f32), _want(topk_gate, "topk_gate", (T, k), f32)
+    _want(topk_idx, "topk_idx", (T, k), torch.int32)
+    _want(x, "x", (T, d), x.dtype), _want(w_router, "w_router", (E, d), x.dtype)
     _want(logits, "logits", (T, E), f32), _want(grad_coef, "grad_coef", (S, E), f32)
     _want(alive, "alive", (E,), torch.uint8)
     _scalar(dloss, "dloss")
-    if data:
-        if dx is None:   # overwritten whole unless accumulated onto
-            dx = torch.zeros_like(x) if accumulate_dx else torch.empty_like(x)
-    else:
+    if not data:
         dx = None
+    elif dx is None and accumulate_dx:
+        dx = torch.zeros_like(x)
+    else:   # overwritten whole unless accumulated onto
+        dx = _out(dx, "dx", (T, d), x.dtype, dev)
     if weights:
         dw_router = _out(dw_router, "dw_router", (E, d), f32, dev)
-        if want_dbias:
+        if want_dbias or dbias is not None:
             dbias = _out(dbias, "dbias", (E,), f32, dev)
     else:
         dw_router, dbias = None, None

@@ -48,3 +48,34 @@ def test_host_and_strided_workspaces_are_refused():
     for call in _calls_with_workspace(z(1 << 20)):        # of any type
         call()
     torch.cuda.synchronize()
+
+
+def _route_bwd_args(T=4, d=64, E=8, k=2):
+    return dict(dgate=z(T, k), topk_idx=z(T, k, dt=I32), topk_gate=z(T, k), logits=z(T, E),
+                x=z(T, d, dt=BF16), w_router=z(E, d, dt=BF16), grad_coef=z(1, E))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,bad", [
+    ("dgate", lambda: z(4, 3)), ("dgate", lambda: z(4, 2, dt=BF16)),
+    ("topk_gate", lambda: z(3, 2)), ("topk_idx", lambda: z(4, 2, dt=torch.int64)),
+    ("x", lambda: z(3, 64, dt=BF16)), ("x", lambda: z(4, 32, dt=BF16)),
+    ("w_router", lambda: z(8, 64)),
+    ("dx", lambda: z(4, 64)), ("dx", lambda: z(3, 64, dt=BF16)),
+    ("dx", lambda: z(4, 128, dt=BF16)[:, :64]),
+    ("dx", lambda: torch.zeros((4, 64), dtype=BF16)),
+    ("dbias", lambda: z(7)), ("dbias", lambda: z(8, dt=BF16)),
+    ("dbias", lambda: torch.zeros(8))])
+def test_router_backward_with_balance_refuses_other_buffers(name, bad):
+    args = _route_bwd_args()
+    args[name] = bad()
+    with pytest.raises(ValueError, match=f"^{name} must"):
+        laep.moe_route_bwd_balance(**args)
+
+
+@pytest.mark.gpu
+def test_router_backward_with_balance_takes_its_own_buffers():
+    args = _route_bwd_args()
+    dx, db = z(4, 64, dt=BF16) + 1, z(8) + 1
+    got = laep.moe_route_bwd_balance(**args, dx=dx, dbias=db)   # a given dbias is computed
+    assert got[0] is dx and got[2] is db and not dx.any() and not db.any()
