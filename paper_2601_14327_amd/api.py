@@ -770,27 +770,28 @@ def moe_grouped_ffn_bwd_gather_act8(dy_perm, x, row_src, k: int, act_q, act_scal
     """moe_grouped_ffn_bwd_gather at pre-activations kept in 8 bits (act_q [R, 2f],
     act_scale [R, 2f/32]); dW_d takes the H recomputed there.  Returns as
     moe_grouped_ffn_bwd."""
-    for t, n in ((x, "x"), (row_src, "row_src"), (w_gate_up, "w_gate_up"), (w_down, "w_down"),
-                 (offsets, "offsets")):
-        _dev(t, n)
+    _dev(x, "x")
+    T, d = x.shape
+    R = row_src.shape[0]
+    n, _, f = w_down.shape
+    E = offsets.shape[0] - 1
+    dev = x.device
+    f32, i32 = torch.float32, torch.int32
     if dy_perm is None:
         if dout is None or topk_gate is None:
             raise ValueError("without dy_perm, dout and topk_gate are needed")
-        _dev(dout, "dout"), _dev(topk_gate, "topk_gate")
+        _want(dout, "dout", (T, d), x.dtype), _want(topk_gate, "topk_gate", (T, k), f32)
     else:
-        _dev(dy_perm, "dy_perm")
-    T, d = x.shape
-    R = row_src.shape[0]
-    f = w_down.shape[2]
-    E = offsets.shape[0] - 1
-    dev = x.device
+        _want(dy_perm, "dy_perm", (R, d), x.dtype)
+    _want(row_src, "row_src", (R,), i32), _want(offsets, "offsets", (E + 1,), i32)
+    _want(expert_map, "expert_map", (E,), i32)
+    _want(w_gate_up, "w_gate_up", (n, 2 * f, d), x.dtype)
+    _want(w_down, "w_down", (n, d, f), x.dtype)
     _want(act_q, "act_q", (R, 2 * f), torch.int8)
     _want(act_scale, "act_scale", (R, 2 * f // LAEP_ACT8_BLOCK), torch.uint8)
-    dx_perm = torch.empty((R, d), dtype=x.dtype, device=dev) if dx_perm is None else dx_perm
-    if dw_gate_up is None:
-        dw_gate_up = torch.empty(w_gate_up.shape, dtype=torch.float32, device=dev)
-    if dw_down is None:
-        dw_down = torch.empty(w_down.shape, dtype=torch.float32, device=dev)
+    dx_perm = _out(dx_perm, "dx_perm", (R, d), x.dtype, dev)
+    dw_gate_up = _out(dw_gate_up, "dw_gate_up", w_gate_up.shape, f32, dev)
+    dw_down = _out(dw_down, "dw_down", w_down.shape, f32, dev)
     ws = _given_ws(ws, dev, LAEP_CALL_FFN_BWD, R, 1, E, d, f)
     check(lib().moe_grouped_ffn_bwd_gather_act8(
         _ptr(dy_perm), _ptr(dout), _ptr(topk_gate), _ptr(x), _ptr(row_src), T, k, _ptr(act_q),

@@ -79,3 +79,52 @@ def test_router_backward_with_balance_takes_its_own_buffers():
     dx, db = z(4, 64, dt=BF16) + 1, z(8) + 1
     got = laep.moe_route_bwd_balance(**args, dx=dx, dbias=db)   # a given dbias is computed
     assert got[0] is dx and got[2] is db and not dx.any() and not db.any()
+
+
+def _expert_bwd_args(T=4, d=64, E=2, k=1, f=64):
+    R = T * k
+    return dict(dy_perm=z(R, d, dt=BF16), x=z(T, d, dt=BF16),
+                row_src=torch.arange(R, dtype=I32, device="cuda"), k=k,
+                act_q=z(R, 2 * f, dt=torch.int8), act_scale=z(R, 2 * f // 32, dt=U8) + 120,
+                w_gate_up=z(E, 2 * f, d, dt=BF16), w_down=z(E, d, f, dt=BF16),
+                offsets=torch.tensor([0, 1, R], dtype=I32, device="cuda"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,bad", [
+    ("dy_perm", lambda: z(4, 64)), ("dy_perm", lambda: z(3, 64, dt=BF16)),
+    ("row_src", lambda: z(4, dt=torch.int64)), ("offsets", lambda: z(3, dt=torch.int64)),
+    ("w_gate_up", lambda: z(2, 128, 64)), ("w_gate_up", lambda: z(2, 64, 64, dt=BF16)),
+    ("w_gate_up", lambda: z(1, 128, 64, dt=BF16)), ("w_down", lambda: z(2, 64, 64)),
+    ("w_down", lambda: z(2, 128, 64, dt=BF16)),
+    ("expert_map", lambda: z(3, dt=I32)), ("expert_map", lambda: z(2, dt=torch.int64)),
+    ("dx_perm", lambda: z(4, 64)), ("dx_perm", lambda: z(4, 128, dt=BF16)[:, :64]),
+    ("dx_perm", lambda: torch.zeros((4, 64), dtype=BF16)),
+    ("dw_gate_up", lambda: z(2, 128, 64, dt=BF16)), ("dw_gate_up", lambda: z(2, 64, 64)),
+    ("dw_down", lambda: z(1, 64, 64)), ("dw_down", lambda: torch.zeros((2, 64, 64)))])
+def test_expert_backward_at_a_checkpoint_refuses_other_buffers(name, bad):
+    args = _expert_bwd_args()
+    args[name] = bad()
+    with pytest.raises(ValueError, match=f"^{name} must"):
+        laep.moe_grouped_ffn_bwd_gather_act8(**args)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,bad", [
+    ("dout", lambda: z(4, 64)), ("dout", lambda: z(3, 64, dt=BF16)),
+    ("topk_gate", lambda: z(4, 1, dt=BF16)), ("topk_gate", lambda: z(4, 2))])
+def test_expert_backward_at_a_checkpoint_refuses_other_gradients(name, bad):
+    args = _expert_bwd_args()
+    args.update(dy_perm=None, dout=z(4, 64, dt=BF16), topk_gate=z(4, 1))
+    args[name] = bad()
+    with pytest.raises(ValueError, match=f"^{name} must"):
+        laep.moe_grouped_ffn_bwd_gather_act8(**args)
+
+
+@pytest.mark.gpu
+def test_expert_backward_at_a_checkpoint_takes_its_own_buffers():
+    args = _expert_bwd_args()
+    own = dict(dx_perm=z(4, 64, dt=BF16) + 1, dw_gate_up=z(2, 128, 64) + 1,
+               dw_down=z(2, 64, 64) + 1)
+    got = laep.moe_grouped_ffn_bwd_gather_act8(**args, **own)
+    assert all(a is b and not a.any() for a, b in zip(got, own.values()))
