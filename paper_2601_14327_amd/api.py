@@ -158,8 +158,8 @@ def moe_route_count(x: torch.Tensor, w_router: torch.Tensor, k: int, *, bias=Non
     dest_row = torch.empty(T * k, dtype=i32, device=dev) if dest_row is None else dest_row
     if want_row_src and row_src is None:
         row_src = torch.empty(T * k, dtype=i32, device=dev)
-    if want_logits and logits is None:
-        logits = torch.empty((T, E), dtype=torch.float32, device=dev)
+    if want_logits or logits is not None:
+        logits = _out(logits, "logits", (T, E), torch.float32, dev)
     ws = _workspace(ws, workspace_bytes(LAEP_CALL_COUNTS, T, k, E), dev)
     check(lib().moe_route_count(_ptr(x), _ptr(w_router), _ptr(bias), _ptr(alive), _dtype_code(x),
                                 T, d, E, k, int(renorm), _ptr(logits), _ptr(topk_idx),

@@ -128,3 +128,21 @@ def test_expert_backward_at_a_checkpoint_takes_its_own_buffers():
                dw_down=z(2, 64, 64) + 1)
     got = laep.moe_grouped_ffn_bwd_gather_act8(**args, **own)
     assert all(a is b and not a.any() for a, b in zip(got, own.values()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [lambda: z(3, 8), lambda: z(4, 8, dt=BF16), lambda: z(8, 4).t(),
+                                 lambda: z(4, 7), lambda: torch.zeros((4, 8))])
+def test_routing_refuses_other_logits(bad):
+    x, wr = z(4, 64, dt=BF16), z(8, 64, dt=BF16)
+    with pytest.raises(ValueError, match="^logits must"):
+        laep.moe_route_count(x, wr, 2, logits=bad())
+    with pytest.raises(ValueError, match="^logits must"):
+        laep.moe_route_count(x, wr, 2, want_logits=True, logits=bad())
+
+
+@pytest.mark.gpu
+def test_routing_writes_given_logits():
+    x, wr = z(4, 64, dt=BF16), z(8, 64, dt=BF16)
+    logits = z(4, 8) + 1
+    assert laep.moe_route_count(x, wr, 2, logits=logits)[6] is logits and not logits.any()
