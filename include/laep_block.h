@@ -145,10 +145,11 @@ int moe_route_bwd_balance(const float* dgate, const int32_t* topk_idx,
  *   b = max(biased exponent of the block's largest magnitude - 6, 1)
  *   scale[r, c / 32] = b;  q[r, c] = clamp(round(act 2^(127 - b)), -127, 127)
  *   (ties to even); the value it stands for is q * 2^(b - 127).
- *   The largest magnitude takes 64 to 127 steps, so the error is at most half
- *   a step, 1/128 of it (float32 magnitudes that round past 127 steps: under
- *   one step).  Decoded values are exact in bf16.  A block that holds an
- *   infinity or a NaN gets b = 255 and decodes to NaNs.
+ *   From 2^-120 up the largest magnitude takes 64 to 127 steps, so the error is
+ *   at most half a step, 1/128 of it (float32 magnitudes that round past 127
+ *   steps: under one step); below 2^-120 steps are 2^-126 and the error at most
+ *   2^-127, however small the block.  Decoded values are exact in bf16.  A block
+ *   that holds an infinity or a NaN gets b = 255 and decodes to NaNs.
  *
  *   act device [R, C] dtype; q device [R, C] int8; scale device [R, C / 32]
  *   uint8.  C % 32 == 0, 0 <= R < 2^31.

@@ -5,9 +5,10 @@
 //   q = clamp(round(v 2^(127 - b)), -127, 127),  the value it stands for q 2^(b - 127).
 // Scaling by a power of two is exact, so rounding happens once, to the nearest of
 // 127 steps (ties to even), and the decoded value is exact in bf16: |q| has 7
-// bits.  The largest magnitude takes 64 to 127 steps, so the error is at most half
-// a step, 1/128 of it (magnitudes above 127.5 steps, which no bf16 value is, lose
-// up to one).  A block with an infinity or a NaN has b = 255 and decodes to NaNs.
+// bits.  From 2^-120 up the largest magnitude takes 64 to 127 steps, so the error is at
+// most half a step, 1/128 of it (magnitudes above 127.5 steps, which no bf16 value is,
+// lose up to one); below 2^-120 steps are 2^-126 and the error at most 2^-127.  A block
+// with an infinity or a NaN has b = 255 and decodes to NaNs.
 #include "common.hpp"
 #include "internal.hpp"
 
