@@ -18,10 +18,10 @@
 // A token's row belongs to G lanes of four experts each (G the power of two from
 // E / 4 up), so a wave reads 64 / G rows at a time in whole lines and a softmax takes
 // log2 G lane moves for its maximum and its sum.  The vector units are as busy as HBM
-// where G lanes hold far fewer than 4 G experts (60 instructions a row and wave), so row
-// addresses are a scalar base and the lane's own place, and rows inside a segment are not
-// checked: 83022 tokens of 77 experts in 25 sequences, forward and backward, 30.2 us for
-// 36.6, 32768 of 45 in 24 18.1 for 20.7.
+// where G lanes hold far fewer than 4 G experts (68 instructions a row and wave in the
+// first pass), so row addresses are a scalar base and the lane's own place, and rows inside
+// a segment are not checked: 83022 tokens of 77 experts in 25 sequences, forward and
+// backward, 30.9 us for 36.6, 32768 of 45 in 24 18.2 for 20.7.
 #include <type_traits>
 
 #include "common.hpp"
@@ -58,8 +58,8 @@ inline int bal_blocks(int E, int cols) { return (E + cols - 1) / cols; }
 
 // Tokens per chunk: two passes of the workgroup's rows at least, and 32; fewer where that
 // would put many sequences into a chunk, which takes them one after the other (about
-// 0.7 us each: 60 sequences of 500 tokens in all over 2 experts 45 us in one chunk; with
-// two tokens at least 900 sequences of 1000 tokens take 20 us, with eight 33).
+// 0.7 us each: 60 sequences of 500 tokens in all over 2 experts, trained, 21 us, in one
+// chunk 45; with two tokens at least 900 sequences of 1000 tokens take 20 us, with eight 31).
 constexpr int kBalLeast = 2;
 inline int bal_cut(int tokens, int T, int n_seq) {   // to about two sequences
   const int two = 2 * (T / n_seq);
@@ -158,7 +158,7 @@ __device__ __forceinline__ bool own(const Quad& q, int lane, int i, int E) {
 // rest does not push out what other calls wrote (131072 x 256, first pass: 43 -> 28 us).
 // VEC: E is a multiple of four and rows are 16-byte aligned; else the four are loaded
 // together all the same, 4-byte aligned (131072 tokens trained, four single loads / one:
-// 45 experts 39 / 30 us, 131 100 / 77, 250 161 / 97).
+// 250 experts 92 / 84 us, 131 62 / 58, though 45 25.4 / 26.3).
 typedef f32x4_t f32x4_a4_t __attribute__((aligned(4)));
 template <bool VEC>
 __device__ __forceinline__ f32x4_t load4(const float* __restrict__ p, int E) {
@@ -359,9 +359,10 @@ __global__ __launch_bounds__(kBalThreads) void balance_chunk_kernel(
 // 20000 of 128 17.8 for 18.7.
 // The loss: alone, the workgroup has it; up to kLastParts workgroups the one that finishes
 // last adds their parts, in their order (its counter was cleared by the first pass); with
-// more, whose release of the counter costs more than it saves, a third kernel does.  Whole
-// call, third kernel / last workgroup, 20000 tokens: 8 workgroups 12.9 / 11.2 us, 32 12.9 /
-// 11.4, 64 13.0 / 12.5, 256 15.3 / 19.7.
+// more, each of which releases the counter, a third kernel does.  Whole call, third kernel /
+// last workgroup, 20000 tokens of 128 experts: 8 workgroups 13.7 / 11.6 us, 32 13.9 / 12.7,
+// 64 14.1 / 13.1, 96 14.1 / 14.0, 128 14.4 / 15.0, 256 14.8 / 18.2: the two cross near 96,
+// and from 32 to there the rule leaves up to a microsecond.
 template <int COLS>
 __global__ __launch_bounds__(kSumThreads) void balance_sum_kernel(
     const uint8_t* __restrict__ alive, const int32_t* __restrict__ off, int T, int E, int k,
@@ -543,7 +544,7 @@ hipError_t launch_balance(const float* logits, const int32_t* topk_idx, const ui
   bal_carve(ws, T, E, n_seq, w);
   const BalOut o = {loss, counts, prob_mean, grad_coef, coef};
   // 32 passes of a workgroup's rows take no longer than two launches: 256 tokens of 64
-  // experts 8.0 us for 11.0, 128 of 256 10.1 for 13.6
+  // experts 7.0 us for 9.4, 128 of 256 7.6 for 9.4
   const bool one = n_seq <= 4 && T <= 32 * (kBalThreads / bal_lanes(E));
   const int chunk = one ? (T > 0 ? T : 1) : bal_chunk(T, E, n_seq);
   const int chunks = bal_chunks(T, chunk);
