@@ -83,12 +83,21 @@ class MoEBlockPlan:
             self.ws_norm = new(max(1, api.workspace_bytes(LAEP_CALL_LAYER_NORM_BWD, T, 1, 1,
                                                           d_model)), dtype=torch.uint8)
 
+    def _check(self, weights: BlockWeights):
+        """The matrices' shapes are the plan's (any number of expert slots: expert_map
+        says which); the layer's calls read them by the plan's sizes."""
+        p, bf16, slots = self.layer, torch.bfloat16, weights.w_down.shape[0]
+        api._want(weights.w_router, "w_router", (p.E, p.d), bf16)
+        api._want(weights.w_gate_up, "w_gate_up", (slots, 2 * p.f, p.d), bf16)
+        api._want(weights.w_down, "w_down", (slots, p.d, p.f), bf16)
+
     def forward(self, x, weights: BlockWeights, residual=None, *, bias=None, alive=None,
                 seq_offsets=None, expert_map=None, etn_accum=None):
         """Returns (out, s); without a residual s is x, which must then keep its values
         until the backward pass.  ``alive``: the router's mask of unpruned experts;
         ``seq_offsets``: int32 [n_seq + 1] on the device, with n_seq > 1."""
         p = self.layer
+        self._check(weights)
         y, s, _, _ = api.moe_layer_norm(x, weights.gamma, weights.beta, residual=residual,
                                         eps=self.eps, out=self.y, mean=self.mean, rstd=self.rstd,
                                         sum_out=None if residual is None else self.sum)
@@ -113,6 +122,8 @@ class MoEBlockPlan:
         layer's dw_router, dbias, dw_gate_up and dw_down (``accumulate`` adds to the
         last two)."""
         p = self.layer
+        self._check(weights)
+        api._want(dout, "dout", (p.T, p.d), torch.bfloat16)
         balance = dict(logits=self.logits, grad_coef=self.grad_coef, alive=self._alive,
                        seq_offsets=self._seq_offsets, dloss=dloss, renorm=self.renorm)
         p.backward(dout, weights.w_gate_up, weights.w_down, expert_map=expert_map,

@@ -146,3 +146,37 @@ def test_routing_writes_given_logits():
     x, wr = z(4, 64, dt=BF16), z(8, 64, dt=BF16)
     logits = z(4, 8) + 1
     assert laep.moe_route_count(x, wr, 2, logits=logits)[6] is logits and not logits.any()
+
+
+def _block():
+    T, d, E, k, f = 8, 64, 4, 2, 64
+    plan = laep.MoEBlockPlan(T, d, E, k, f)
+    w = dict(gamma=z(d) + 1, beta=None, w_router=z(E, d, dt=BF16),
+             w_gate_up=z(E, 2 * f, d, dt=BF16), w_down=z(E, d, f, dt=BF16))
+    return plan, w, z(T, d, dt=BF16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,bad", [
+    ("w_router", lambda: z(4, 32, dt=BF16)), ("w_router", lambda: z(3, 64, dt=BF16)),
+    ("w_router", lambda: z(4, 64)), ("w_gate_up", lambda: z(4, 64, 64, dt=BF16)),
+    ("w_gate_up", lambda: z(3, 128, 64, dt=BF16)), ("w_gate_up", lambda: z(4, 128, 64)),
+    ("w_down", lambda: z(4, 64, 32, dt=BF16)), ("w_down", lambda: z(4, 64, 64))])
+def test_block_refuses_weights_of_other_sizes(name, bad):
+    plan, w, x = _block()
+    plan.forward(x, laep.BlockWeights(**w))
+    wrong = laep.BlockWeights(**dict(w, **{name: bad()}))
+    for call in (lambda: plan.forward(x, wrong), lambda: plan.backward(x, wrong)):
+        with pytest.raises(ValueError, match=f"^{name} must"):
+            call()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [lambda: z(7, 64, dt=BF16), lambda: z(8, 64),
+                                 lambda: z(8, 128, dt=BF16)[:, ::2],
+                                 lambda: torch.zeros((8, 64), dtype=BF16)])
+def test_block_refuses_other_gradients(bad):
+    plan, w, x = _block()
+    plan.forward(x, laep.BlockWeights(**w))
+    with pytest.raises(ValueError, match="^dout must"):
+        plan.backward(bad(), laep.BlockWeights(**w))
