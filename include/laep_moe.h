@@ -70,6 +70,8 @@ extern "C" {
 #define LAEP_CALL_ROUTE_BWD 4
 #define LAEP_CALL_LAYER_NORM_BWD 5 /* laep_block.h; (T, 1, 1, d_model, 0) */
 #define LAEP_CALL_BALANCE 6        /* laep_block.h; (T, n_seq, E, 0, 0)   */
+#define LAEP_CALL_MX4_PRODUCT 7    /* laep_mx4.h; (T, k, E, K, N)         */
+#define LAEP_CALL_MX4_FFN 8        /* laep_mx4.h; (T, k, E, d_model, d_ff) */
 
 /* Limits of the library. */
 #define LAEP_MAX_EXPERTS 256

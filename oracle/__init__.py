@@ -17,10 +17,11 @@ laep      the LAEP prune rule (Section 3.2, Eqs. (1)-(2); Appendix,
           Algorithm 2)
 block     layer norm, balance loss and 8-bit activation checkpoints around
           the layer, and their backward
+mx4       microscaled 4-bit matrices and the products at them
 
 Pins (tests marked ``not gpu``) tie every function to something other than
 itself: brute-force enumeration, invariants, closed forms, finite
 differences, an independent autograd evaluation and hand-worked examples.
 Functions without such a pin say "parity unpinned" in their docstring.
 """
-from . import numerics, moe, laep, block  # noqa: F401
+from . import numerics, moe, laep, block, mx4  # noqa: F401

@@ -30,14 +30,25 @@ and what a pre-norm MoE block computes around them:
                          the SwiGLU and the whole expert backward at them
     MoEBlockPlan         all of it as one training step of a pre-norm block
 
+and experts in microscaled 4 bits (MX4; Mx4 holds a matrix's codes and scales):
+
+    moe_mx4_quantize, moe_mx4_dequantize    matrices to MX4 and back
+    moe_mx4_grouped_product                 routed rows (MX4 or bf16) times their expert's
+                         MX4 matrix
+    moe_grouped_ffn_fwd_mx4                 the SwiGLU expert FFN at MX4 weights, activations
+                         in MX4 or bf16; MoELayerPlan and MoEBlockPlan run it when they are
+                         given weights in MX4
+
     laep_calib_copy, laep_calib_read,  measurement calls (attained peaks,
     laep_calib_mfma                    the router's feed bound)
     laep_ffn_fwd_row_tile              which kernels a forward call runs
 """
 from ._lib import (  # noqa: F401
     LAEP_ACT8_BLOCK, LAEP_BF16, LAEP_CALL_BALANCE, LAEP_CALL_FFN_BWD, LAEP_CALL_FFN_FWD,
-    LAEP_CALL_LAYER_NORM_BWD, LAEP_F32, LaepError, LIB_PATH, lib)
+    LAEP_CALL_LAYER_NORM_BWD, LAEP_CALL_MX4_FFN, LAEP_CALL_MX4_PRODUCT, LAEP_F32, LAEP_MX4_BLOCK,
+    LAEP_MX4_GROUP, LaepError, LIB_PATH, lib)
 from .api import (  # noqa: F401
+    Mx4,
     ffn_bwd_ws_views,
     ffn_fwd_h_view,
     laep_calib_copy,
@@ -62,8 +73,12 @@ from .api import (  # noqa: F401
     moe_grouped_ffn_fwd,
     moe_grouped_ffn_fwd_gather,
     moe_grouped_ffn_fwd_gather_combine,
+    moe_grouped_ffn_fwd_mx4,
     moe_layer_norm,
     moe_layer_norm_bwd,
+    moe_mx4_dequantize,
+    moe_mx4_grouped_product,
+    moe_mx4_quantize,
     moe_permute,
     moe_permute_bwd,
     moe_route,

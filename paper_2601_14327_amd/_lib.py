@@ -22,8 +22,12 @@ LAEP_CALL_FFN_BWD = 3
 LAEP_CALL_ROUTE_BWD = 4
 LAEP_CALL_LAYER_NORM_BWD = 5
 LAEP_CALL_BALANCE = 6
+LAEP_CALL_MX4_PRODUCT = 7
+LAEP_CALL_MX4_FFN = 8
 
 LAEP_ACT8_BLOCK = 32    # columns that share a scale of an 8-bit checkpoint
+LAEP_MX4_BLOCK = 32     # columns that share a scale of an MX4 matrix
+LAEP_MX4_GROUP = 256    # columns whose scales lie together
 
 ERROR_NAMES = {
     1: "LAEP_ERR_INVALID_ARG",
@@ -93,6 +97,13 @@ SIGNATURES = {
     "moe_act8_save": (_i, [_p, _i, _i64, _i, _p, _p, _p]),
     "moe_act8_load": (_i, [_p, _p, _i, _i64, _i, _p, _p]),
     "moe_swiglu_bwd_act8": (_i, [_p, _p, _p, _i, _i64, _i, _p, _p, _p]),
+    # experts in microscaled 4 bits (laep_mx4.h)
+    "moe_mx4_quantize": (_i, [_p, _i, _i, _i64, _i, _p, _p, _p]),
+    "moe_mx4_dequantize": (_i, [_p, _p, _i, _i, _i64, _i, _p, _p]),
+    "moe_mx4_grouped_product": (_i, [_p, _p, _p, _i, _i, _p, _p, _p, _p, _i, _i, _i, _i, _i64, _p,
+                                     _p, _sz, _p]),
+    "moe_grouped_ffn_fwd_mx4": (_i, [_p, _p, _i, _i, _p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i64,
+                                     _p, _p, _p, _sz, _p]),
     # measurement calls (laep_calib.h)
     "laep_calib_copy": (_i, [_p, _p, _sz, _p]),
     "laep_calib_mfma": (_i, [_i, _i, _p, _p]),

@@ -9,13 +9,14 @@ from __future__ import annotations
 
 import ctypes
 import math
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
 from ._lib import (LAEP_ACT8_BLOCK, LAEP_BF16, LAEP_CALL_BALANCE, LAEP_CALL_COUNTS,
                    LAEP_CALL_FFN_BWD, LAEP_CALL_FFN_FWD, LAEP_CALL_LAYER_NORM_BWD,
-                   LAEP_CALL_ROUTE_BWD, LAEP_F32, LaepError, check, lib)
+                   LAEP_CALL_MX4_FFN, LAEP_CALL_MX4_PRODUCT, LAEP_CALL_ROUTE_BWD, LAEP_F32,
+                   LAEP_MX4_BLOCK, LAEP_MX4_GROUP, LaepError, check, lib)
 
 _DT = {torch.float32: LAEP_F32, torch.bfloat16: LAEP_BF16}
 
@@ -800,6 +801,160 @@ def moe_grouped_ffn_bwd_gather_act8(dy_perm, x, row_src, k: int, act_q, act_scal
         int(accumulate), _ptr(ws), ws.numel() * ws.element_size(), _stream(dev)))
     out = (dx_perm, dw_gate_up, dw_down)
     return out + (ws,) if return_ws else out
+
+
+# ---- experts in microscaled 4 bits (laep_mx4.h) ----------------------------------------
+class Mx4(NamedTuple):
+    """A matrix [..., R, C] in microscaled 4 bits, as moe_mx4_quantize writes it: codes
+    uint8 [..., R, C / 2], scale uint8 [..., ceil(C / 256), R, 8]."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+
+
+def _mx4_scale_shape(R: int, C: int):
+    return (-(-C // LAEP_MX4_GROUP), R, LAEP_MX4_GROUP // LAEP_MX4_BLOCK)
+
+
+def _want_mx4(w, name: str, shape, device):
+    """A given Mx4 of this matrix shape, on this device."""
+    if not isinstance(w, Mx4):
+        raise ValueError(f"{name} must be an Mx4 (moe_mx4_quantize's codes and scale)")
+    lead = tuple(shape[:-2])
+    _want(w.codes, f"{name}.codes", lead + (shape[-2], shape[-1] // 2), torch.uint8)
+    _want(w.scale, f"{name}.scale", lead + _mx4_scale_shape(*shape[-2:]), torch.uint8)
+    _same_device(device, **{f"{name}.codes": w.codes, f"{name}.scale": w.scale})
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, not {device}")
+
+
+def _on_device(device, fn, *args):
+    """check(fn(*args)) with the tensors' device current: the C calls launch there."""
+    if torch.cuda.current_device() == device.index:
+        check(fn(*args))
+    else:
+        with torch.cuda.device(device):
+            check(fn(*args))
+
+
+def moe_mx4_quantize(src: torch.Tensor, *, codes=None, scale=None) -> Mx4:
+    """The matrices src [..., R, C] (bf16 or float32, C a multiple of 32) in
+    microscaled 4 bits: every 32 columns of a row share a power-of-two scale."""
+    _dev(src, "src")
+    if src.dim() < 2:
+        raise ValueError("src must have rows and columns")
+    lead, (R, C) = tuple(src.shape[:-2]), src.shape[-2:]
+    code = _dtype_code(src)
+    codes = _out(codes, "codes", lead + (R, C // 2), torch.uint8, src.device)
+    scale = _out(scale, "scale", lead + _mx4_scale_shape(R, C), torch.uint8, src.device)
+    _same_device(src.device, codes=codes, scale=scale)
+    _on_device(src.device, lib().moe_mx4_quantize, _ptr(src), code, math.prod(lead), R, C,
+               _ptr(codes), _ptr(scale), _stream(src.device))
+    return Mx4(codes, scale)
+
+
+def moe_mx4_dequantize(codes: torch.Tensor, scale: torch.Tensor,
+                       dtype: torch.dtype = torch.bfloat16, *, out=None):
+    """The values [..., R, C] that codes and scale stand for, in dtype (exact)."""
+    _dev(codes, "codes")
+    if codes.dim() < 2:
+        raise ValueError("codes must have rows and columns")
+    lead, R, C = tuple(codes.shape[:-2]), codes.shape[-2], 2 * codes.shape[-1]
+    dev = codes.device
+    if dtype not in _DT:
+        raise LaepError(2, f"unsupported dtype {dtype}")
+    _want(codes, "codes", codes.shape, torch.uint8)
+    _want(scale, "scale", lead + _mx4_scale_shape(R, C), torch.uint8)
+    out = _out(out, "out", lead + (R, C), dtype, dev)
+    _same_device(dev, scale=scale, out=out)
+    _on_device(dev, lib().moe_mx4_dequantize, _ptr(codes), _ptr(scale), _DT[dtype],
+               math.prod(lead), R, C, _ptr(out), _stream(dev))
+    return out
+
+
+def _mx4_routing(dev, T: int, k: int, offsets, row_src, expert_map, slots: int):
+    """Checks of the routing's tensors.  Returns (E, R, k as the C calls take it)."""
+    if offsets.dim() != 1 or offsets.numel() < 2:
+        raise ValueError("offsets must be an int32 tensor [E + 1]")
+    E = offsets.shape[0] - 1
+    _want(offsets, "offsets", (E + 1,), torch.int32)
+    if row_src is not None:
+        _want(row_src, "row_src", (row_src.numel(),), torch.int32)
+    _want(expert_map, "expert_map", (E,), torch.int32)
+    if expert_map is None and slots != E:
+        raise ValueError(f"{slots} weight slots for {E} experts need an expert_map")
+    _same_device(dev, offsets=offsets, row_src=row_src, expert_map=expert_map)
+    return E, (T if row_src is None else row_src.numel()), (1 if row_src is None else k)
+
+
+def moe_mx4_grouped_product(x, w: Mx4, offsets: torch.Tensor, *, row_src=None, k: int = 1,
+                            expert_map=None, dtype: torch.dtype = torch.bfloat16, out=None,
+                            ws=None):
+    """Routed rows times their expert's matrix: out [R, N] in dtype, out[r] =
+    x[row_src[r] // k] @ W[slot].T.  x [T, K] is an Mx4 or bf16; w an Mx4 of [slots, N,
+    K] (N, K multiples of 64); without row_src x's rows are already in the experts'
+    order.  Rows of experts with a negative expert_map entry are left as they were."""
+    mx4 = isinstance(x, Mx4)
+    rows = x.codes if mx4 else x
+    _dev(rows, "x")
+    if rows.dim() != 2 or not isinstance(w, Mx4) or w.codes.dim() != 3:
+        raise ValueError("x must be a matrix [T, K], w an Mx4 of [slots, N, K]")
+    dev = rows.device
+    T, K = rows.shape[0], rows.shape[1] * (2 if mx4 else 1)
+    slots, N = w.codes.shape[:2]
+    _want_mx4(w, "w", (slots, N, K), dev)
+    if mx4:
+        _want_mx4(x, "x", (T, K), dev)
+    else:
+        _want(x, "x", (T, K), torch.bfloat16)
+    if dtype not in _DT:
+        raise LaepError(2, f"unsupported dtype {dtype}")
+    E, R, k = _mx4_routing(dev, T, k, offsets, row_src, expert_map, slots)
+    out = _out(out, "out", (R, N), dtype, dev)
+    ws = _given_ws(ws, dev, LAEP_CALL_MX4_PRODUCT, T, k, E, K, N)
+    _same_device(dev, out=out, ws=ws)
+    _on_device(dev, lib().moe_mx4_grouped_product, _ptr(rows), _ptr(x.scale) if mx4 else None,
+               _ptr(row_src), T, k, _ptr(w.codes), _ptr(w.scale), _ptr(offsets),
+               _ptr(expert_map), _DT[dtype], E, N, K, R, _ptr(out), _ptr(ws),
+               ws.numel() * ws.element_size(), _stream(dev))
+    return out
+
+
+def moe_grouped_ffn_fwd_mx4(x: torch.Tensor, w_gate_up: Mx4, w_down: Mx4,
+                            offsets: torch.Tensor, *, row_src=None, k: int = 1,
+                            act_bits: int = 16, expert_map=None, save_act: bool = False,
+                            act_save=None, y_perm=None, ws=None):
+    """The grouped SwiGLU FFN at weights in microscaled 4 bits (Mx4 of [slots, 2f, d] and
+    [slots, d, f]) over the bf16 tokens x [T, d], routed row r reading token
+    row_src[r] // k (without row_src: row r).  ``act_bits`` 16 keeps X and H in bf16, 4
+    rounds both to MX4.  ``save_act`` (act_bits 16) keeps the pre-activations for
+    moe_grouped_ffn_bwd_gather at moe_mx4_dequantize of the weights.  Returns (y_perm
+    [R, d], act_save [R, 2f] or None)."""
+    _dev(x, "x")
+    if x.dim() != 2 or any(not isinstance(w, Mx4) or w.codes.dim() != 3
+                           for w in (w_gate_up, w_down)):
+        raise ValueError("x must be a matrix [T, d], the weights Mx4 of [slots, ., .]")
+    dev = x.device
+    T, d = x.shape
+    slots, f = w_down.codes.shape[0], 2 * w_down.codes.shape[2]
+    _want(x, "x", (T, d), torch.bfloat16)
+    _want_mx4(w_gate_up, "w_gate_up", (slots, 2 * f, d), dev)
+    _want_mx4(w_down, "w_down", (slots, d, f), dev)
+    E, R, k = _mx4_routing(dev, T, k, offsets, row_src, expert_map, slots)
+    y_perm = _out(y_perm, "y_perm", (R, d), torch.bfloat16, dev)
+    if save_act or act_save is not None:
+        act_save = _out(act_save, "act_save", (R, 2 * f), torch.bfloat16, dev)
+    ws = _given_ws(ws, dev, LAEP_CALL_MX4_FFN, T, k, E, d, f)
+    _same_device(dev, y_perm=y_perm, act_save=act_save, ws=ws)
+    _on_device(dev, lib().moe_grouped_ffn_fwd_mx4, _ptr(x), _ptr(row_src), T, k,
+               _ptr(w_gate_up.codes), _ptr(w_gate_up.scale), _ptr(w_down.codes),
+               _ptr(w_down.scale), _ptr(offsets), _ptr(expert_map), int(act_bits), E, d, f, R,
+               _ptr(y_perm), _ptr(act_save), _ptr(ws), ws.numel() * ws.element_size(),
+               _stream(dev))
+    return y_perm, act_save
 
 
 # ---- measurement calls (laep_calib.h) -------------------------------------------------

@@ -11,6 +11,7 @@
 #include "../../include/laep_moe.h"
 #include "../../include/laep_block.h"
 #include "../../include/laep_calib.h"
+#include "../../include/laep_mx4.h"
 #include "internal.hpp"
 
 namespace {
@@ -122,6 +123,10 @@ size_t moe_workspace_bytes(int which_call, int T, int k, int E, int d_model, int
       return laep::layer_norm_bwd_ws_bytes(T, d_model < 0 ? 0 : d_model);
     case LAEP_CALL_BALANCE:
       return laep::balance_ws_bytes(T, E, k);
+    case LAEP_CALL_MX4_PRODUCT:
+      return laep::mx4_product_ws_bytes(T, k, E, d_model < 0 ? 0 : d_model, d_ff < 0 ? 0 : d_ff);
+    case LAEP_CALL_MX4_FFN:
+      return laep::ffn_fwd_mx4_ws_bytes(T, k, E, d_model < 0 ? 0 : d_model, d_ff < 0 ? 0 : d_ff);
     default:
       return 0;
   }
@@ -883,6 +888,183 @@ int moe_swiglu_bwd_act8(const int8_t* q, const uint8_t* scale, const void* dh, i
   return hip_status(laep::launch_swiglu_bwd_act8(q, scale, dh, dtype, R, d_ff, da, h,
                                                  as_stream(stream)),
                     "moe_swiglu_bwd_act8");
+}
+
+}  // extern "C"
+
+namespace {
+
+int check_mx4_matrix(const char* name, int dtype, int n, int64_t R, int C) {
+  int rc = check_dtype(dtype);
+  if (rc) return rc;
+  REQUIRE(n >= 0, LAEP_ERR_INVALID_ARG, "%s: n=%d < 0", name, n);
+  REQUIRE(R >= 0 && R <= 0x7FFFFFFFll, LAEP_ERR_INVALID_ARG, "%s: R=%lld outside [0, 2^31)", name,
+          (long long)R);
+  REQUIRE(C > 0 && C % LAEP_MX4_BLOCK == 0, LAEP_ERR_INVALID_ARG,
+          "%s: %d columns are not a positive multiple of %d", name, C, LAEP_MX4_BLOCK);
+  return LAEP_OK;
+}
+
+// what the MX4 products share: experts, rows, and one matrix [N, K] of an expert
+int check_mx4_rows(const char* name, const void* row_src, int T, int k, int E, int64_t R) {
+  REQUIRE(E >= 1 && E <= LAEP_MAX_EXPERTS, LAEP_ERR_INVALID_ARG, "%s: E=%d outside [1, %d]", name,
+          E, LAEP_MAX_EXPERTS);
+  REQUIRE(T >= 0 && k >= 1, LAEP_ERR_INVALID_ARG, "%s: T=%d, k=%d", name, T, k);
+  REQUIRE(R >= 0 && R <= 0x7FFFFFFFll, LAEP_ERR_INVALID_ARG, "%s: R=%lld outside [0, 2^31)", name,
+          (long long)R);
+  REQUIRE(R <= (row_src ? (int64_t)T * k : (int64_t)T), LAEP_ERR_INVALID_ARG,
+          "%s: R=%lld exceeds %s", name, (long long)R, row_src ? "T*k" : "T (without row_src)");
+  return LAEP_OK;
+}
+
+int check_mx4_shape(const char* name, int64_t N, int64_t K) {
+  REQUIRE(N > 0 && K > 0, LAEP_ERR_INVALID_ARG, "%s: sizes must be > 0 (got %lld, %lld)", name,
+          (long long)N, (long long)K);
+  REQUIRE(N % 64 == 0 && K % 64 == 0, LAEP_ERR_UNSUPPORTED,
+          "%s: %lld and %lld must be multiples of 64", name, (long long)N, (long long)K);
+  REQUIRE(N * K / 2 < kMaxBufferBytes, LAEP_ERR_UNSUPPORTED,
+          "%s: one expert's codes (%lld x %lld) must be under 2 GiB", name, (long long)N,
+          (long long)K);
+  return LAEP_OK;
+}
+
+// a product's activations [rows, K], addressed with 32-bit byte offsets
+int check_mx4_act(const char* name, int64_t rows, int64_t K, bool mx4) {
+  REQUIRE(rows * K * (mx4 ? 1 : 4) / 2 < kMaxBufferBytes, LAEP_ERR_UNSUPPORTED,
+          "%s: the activations (%lld x %lld) must be under 2 GiB", name, (long long)rows,
+          (long long)K);
+  return LAEP_OK;
+}
+
+size_t mx4_scale_bytes(int64_t R, int64_t C) { return (size_t)((C + 255) / 256) * R * 8; }
+
+}  // namespace
+
+extern "C" {
+
+int moe_mx4_quantize(const void* src, int dtype, int n, int64_t R, int C, uint8_t* codes,
+                     uint8_t* scale, void* stream) {
+  int rc = check_mx4_matrix("moe_mx4_quantize", dtype, n, R, C);
+  if (rc) return rc;
+  if (n == 0 || R == 0) return ok();
+  REQUIRE(src && codes && scale, LAEP_ERR_INVALID_ARG,
+          "moe_mx4_quantize: src, codes and scale must be non-null");
+  REQUIRE(aligned16(src) && aligned16(codes) && aligned16(scale), LAEP_ERR_INVALID_ARG,
+          "moe_mx4_quantize: buffers must be 16-byte aligned");
+  const size_t sb = (size_t)n * R * C * elem_bytes(dtype), cb = (size_t)n * R * C / 2,
+               eb = n * mx4_scale_bytes(R, C);
+  REQUIRE(!overlap(src, sb, codes, cb) && !overlap(src, sb, scale, eb) &&
+              !overlap(codes, cb, scale, eb),
+          LAEP_ERR_INVALID_ARG, "moe_mx4_quantize: src, codes and scale must not overlap");
+  return hip_status(laep::launch_mx4_quantize(src, dtype, n, R, C, codes, scale, as_stream(stream)),
+                    "moe_mx4_quantize");
+}
+
+int moe_mx4_dequantize(const uint8_t* codes, const uint8_t* scale, int dtype, int n, int64_t R,
+                       int C, void* out, void* stream) {
+  int rc = check_mx4_matrix("moe_mx4_dequantize", dtype, n, R, C);
+  if (rc) return rc;
+  if (n == 0 || R == 0) return ok();
+  REQUIRE(codes && scale && out, LAEP_ERR_INVALID_ARG,
+          "moe_mx4_dequantize: codes, scale and out must be non-null");
+  REQUIRE(aligned16(codes) && aligned16(scale) && aligned16(out), LAEP_ERR_INVALID_ARG,
+          "moe_mx4_dequantize: buffers must be 16-byte aligned");
+  const size_t ob = (size_t)n * R * C * elem_bytes(dtype), cb = (size_t)n * R * C / 2,
+               eb = n * mx4_scale_bytes(R, C);
+  REQUIRE(!overlap(out, ob, codes, cb) && !overlap(out, ob, scale, eb), LAEP_ERR_INVALID_ARG,
+          "moe_mx4_dequantize: out must not overlap codes or scale");
+  return hip_status(
+      laep::launch_mx4_dequantize(codes, scale, dtype, n, R, C, out, as_stream(stream)),
+      "moe_mx4_dequantize");
+}
+
+int moe_mx4_grouped_product(const void* x, const uint8_t* x_scale, const int32_t* row_src, int T,
+                            int k, const uint8_t* w, const uint8_t* w_scale,
+                            const int32_t* offsets, const int32_t* expert_map, int out_dtype,
+                            int E, int N, int K, int64_t R, void* out, void* ws, size_t ws_bytes,
+                            void* stream) {
+  const char* const name = "moe_mx4_grouped_product";
+  int rc = check_dtype(out_dtype);
+  if (rc) return rc;
+  if ((rc = check_mx4_rows(name, row_src, T, k, E, R))) return rc;
+  if ((rc = check_mx4_shape(name, N, K))) return rc;
+  if ((rc = check_mx4_act(name, T, K, x_scale != nullptr))) return rc;
+  REQUIRE(offsets, LAEP_ERR_INVALID_ARG, "%s: offsets must be non-null", name);
+  if (R == 0) return ok();
+  const size_t need = laep::mx4_product_ws_bytes(T, k, E, K, N);
+  REQUIRE(x && w && w_scale && out && (ws || need == 0), LAEP_ERR_INVALID_ARG,
+          "%s: x, w, w_scale, out and ws must be non-null", name);
+  REQUIRE(aligned16(x) && aligned16(x_scale) && aligned16(w) && aligned16(w_scale) &&
+              aligned16(out) && aligned16(ws),
+          LAEP_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", name);
+  REQUIRE(ws_bytes >= need, LAEP_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", name, ws_bytes,
+          need);
+  const size_t out_bytes = (size_t)R * N * elem_bytes(out_dtype);
+  const size_t x_bytes = x_scale ? (size_t)T * K / 2 : (size_t)T * K * 2;
+  REQUIRE(!overlap(out, out_bytes, x, x_bytes) &&
+              !overlap(out, out_bytes, x_scale, mx4_scale_bytes(T, K)) &&
+              !overlap(out, out_bytes, w, (size_t)N * K / 2) &&
+              !overlap(out, out_bytes, w_scale, mx4_scale_bytes(N, K)) &&
+              !overlap(out, out_bytes, ws, need),
+          LAEP_ERR_INVALID_ARG, "%s: out must not overlap the inputs or ws", name);
+  return hip_status(laep::launch_mx4_product(x, x_scale, row_src, T, k, w, w_scale, offsets,
+                                             expert_map, out_dtype, E, N, K, R, out, ws,
+                                             as_stream(stream)),
+                    name);
+}
+
+int moe_grouped_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int k,
+                            const uint8_t* w_gate_up, const uint8_t* w_gate_up_scale,
+                            const uint8_t* w_down, const uint8_t* w_down_scale,
+                            const int32_t* offsets, const int32_t* expert_map, int act_bits, int E,
+                            int d_model, int d_ff, int64_t R, void* y_perm, void* act_save,
+                            void* ws, size_t ws_bytes, void* stream) {
+  const char* const name = "moe_grouped_ffn_fwd_mx4";
+  REQUIRE(act_bits == 4 || act_bits == 16, LAEP_ERR_UNSUPPORTED,
+          "%s: act_bits=%d is neither 4 nor 16", name, act_bits);
+  REQUIRE(act_bits == 16 || !act_save, LAEP_ERR_UNSUPPORTED,
+          "%s: act_save needs act_bits=16", name);
+  int rc = check_mx4_rows(name, row_src, T, k, E, R);
+  if (rc) return rc;
+  if ((rc = check_mx4_shape(name, 2 * (int64_t)d_ff, d_model))) return rc;
+  if ((rc = check_mx4_shape(name, d_model, d_ff))) return rc;
+  if ((rc = check_mx4_act(name, T, d_model, false))) return rc;
+  // H's scales are addressed over all rows
+  REQUIRE(act_bits == 16 || mx4_scale_bytes(R, d_ff) < (size_t)kMaxBufferBytes,
+          LAEP_ERR_UNSUPPORTED, "%s: R=%lld rows of d_ff=%d are too many in one call", name,
+          (long long)R, d_ff);
+  REQUIRE(offsets, LAEP_ERR_INVALID_ARG, "%s: offsets must be non-null", name);
+  if (R == 0) return ok();
+  REQUIRE(x && w_gate_up && w_gate_up_scale && w_down && w_down_scale && y_perm && ws,
+          LAEP_ERR_INVALID_ARG,
+          "%s: x, the weights, their scales, y_perm and ws must be non-null", name);
+  REQUIRE(aligned16(x) && aligned16(w_gate_up) && aligned16(w_gate_up_scale) &&
+              aligned16(w_down) && aligned16(w_down_scale) && aligned16(y_perm) &&
+              aligned16(act_save) && aligned16(ws),
+          LAEP_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", name);
+  const size_t need = laep::ffn_fwd_mx4_ws_bytes(T, row_src ? k : 1, E, d_model, d_ff);
+  REQUIRE(ws_bytes >= need, LAEP_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", name, ws_bytes,
+          need);
+  const size_t x_bytes = (size_t)T * d_model * 2, y_bytes = (size_t)R * d_model * 2;
+  const size_t a_bytes = (size_t)R * d_ff * 4;
+  const size_t gu_bytes = (size_t)d_ff * d_model, d_bytes = (size_t)d_ff * d_model / 2;
+  const struct {
+    const void* p;
+    size_t n;
+  } in[] = {{x, x_bytes}, {w_gate_up, gu_bytes}, {w_down, d_bytes}, {ws, need},
+            {w_gate_up_scale, mx4_scale_bytes(2 * (int64_t)d_ff, d_model)},
+            {w_down_scale, mx4_scale_bytes(d_model, d_ff)}};
+  for (const auto& b : in)
+    REQUIRE(!overlap(y_perm, y_bytes, b.p, b.n) && !overlap(act_save, a_bytes, b.p, b.n),
+            LAEP_ERR_INVALID_ARG, "%s: y_perm and act_save must not overlap the inputs or ws",
+            name);
+  REQUIRE(!overlap(y_perm, y_bytes, act_save, a_bytes), LAEP_ERR_INVALID_ARG,
+          "%s: y_perm must not overlap act_save", name);
+  return hip_status(laep::launch_ffn_fwd_mx4(x, row_src, T, k, w_gate_up, w_gate_up_scale, w_down,
+                                             w_down_scale, offsets, expert_map, act_bits, E,
+                                             d_model, d_ff, R, y_perm, act_save, ws,
+                                             as_stream(stream)),
+                    name);
 }
 
 // ---- measurement calls (laep_calib.h) --------------------------------------------

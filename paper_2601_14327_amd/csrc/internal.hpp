@@ -168,6 +168,24 @@ hipError_t launch_act8_load(const void* q, const uint8_t* scale, int dtype, int6
 hipError_t launch_swiglu_bwd_act8(const void* q, const uint8_t* scale, const void* dh, int dtype,
                                   int64_t R, int f, void* da, void* h, hipStream_t s);
 
+// MX4 matrices (n of [R, C]): codes [n, R, C / 2], scale [n, ceil(C / 256), R, 8].
+hipError_t launch_mx4_quantize(const void* src, int dtype, int n, int64_t R, int C, uint8_t* codes,
+                               uint8_t* scale, hipStream_t s);
+hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scale, int dtype, int n,
+                                 int64_t R, int C, void* out, hipStream_t s);
+// Products at MX4 weights; x_scale NULL: x is bf16; row_src NULL: rows in order.
+size_t mx4_product_ws_bytes(int T, int k, int E, int K, int N);
+hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32_t* row_src, int T,
+                              int k, const uint8_t* w, const uint8_t* w_scale,
+                              const int32_t* offsets, const int32_t* expert_map, int out_dtype,
+                              int E, int N, int K, int64_t R, void* out, void* ws, hipStream_t s);
+size_t ffn_fwd_mx4_ws_bytes(int T, int k, int E, int d, int f);
+hipError_t launch_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int k,
+                              const uint8_t* w_gu, const uint8_t* w_gu_scale, const uint8_t* w_d,
+                              const uint8_t* w_d_scale, const int32_t* offsets,
+                              const int32_t* expert_map, int act_bits, int E, int d, int f,
+                              int64_t R, void* y_perm, void* act_save, void* ws, hipStream_t s);
+
 // Measurement kernels (laep_calib.h).
 hipError_t launch_calib_copy(const void* src, void* dst, size_t bytes, hipStream_t s);
 hipError_t launch_calib_mfma(int n_workgroups, int iters, float* out, hipStream_t s);
