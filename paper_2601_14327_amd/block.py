@@ -21,7 +21,7 @@ model can share (``scratch``), since their passes run one after the other.
 """
 from __future__ import annotations
 
-from typing import NamedTuple, Optional
+from typing import NamedTuple, Optional, Union
 
 import torch
 
@@ -32,26 +32,29 @@ from .layer import MoELayerPlan
 
 class BlockWeights(NamedTuple):
     """gamma, beta float32 [d] (beta may be None); w_router [E, d], w_gate_up
-    [E, 2f, d] and w_down [E, d, f] in the plan's dtype."""
+    [E, 2f, d] and w_down [E, d, f] in the plan's dtype (the last two api.Mx4 where it
+    has mx4_act)."""
     gamma: torch.Tensor
     beta: Optional[torch.Tensor]
     w_router: torch.Tensor
-    w_gate_up: torch.Tensor
-    w_down: torch.Tensor
+    w_gate_up: Union[torch.Tensor, api.Mx4]
+    w_down: Union[torch.Tensor, api.Mx4]
 
 
 class MoEBlockPlan:
     def __init__(self, T: int, d_model: int, E: int, k: int, d_ff: int, *, n_seq: int = 1,
                  coef: float = 0.01, eps: float = 1e-5, renorm: bool = True,
                  training: bool = True, act_bits: int = 8, device="cuda",
-                 scratch: Optional["MoEBlockPlan"] = None):
+                 scratch: Optional["MoEBlockPlan"] = None, mx4_act: Optional[int] = None):
         """``coef`` weighs the balance loss, over the batch (n_seq = 1) or per
         sequence; ``training`` False keeps nothing for a backward pass;
         ``act_bits``: how a training block keeps its pre-activations.  8 (the default)
         takes a third of the memory of 16 and 4 % more time a step, and the expert
         backward then sees them rounded to 1/128 of the largest of 32 neighbours; 16
         keeps them, and H, as the forward computed them.
-        ``scratch``: a block of the same sizes whose transient buffers to use."""
+        ``scratch``: a block of the same sizes whose transient buffers to use.
+        ``mx4_act`` 4 or 16 (``training`` False): the expert weights are in microscaled 4
+        bits, the experts' activations in that many."""
         if scratch is not None and scratch.n_seq != n_seq:
             raise ValueError("scratch must be a block of the same sizes and kind")
         bf16, f32 = torch.bfloat16, torch.float32
@@ -59,7 +62,8 @@ class MoEBlockPlan:
         self.training = training
         self.layer = MoELayerPlan(T, d_model, E, k, d_ff, dtype=bf16, device=device,
                                   backward=training, act_bits=act_bits if training else 16,
-                                  scratch=None if scratch is None else scratch.layer)
+                                  scratch=None if scratch is None else scratch.layer,
+                                  mx4_act=mx4_act)
         dev = self.layer.device
 
         def new(*shape, dtype=f32):
@@ -86,8 +90,15 @@ class MoEBlockPlan:
     def _check(self, weights: BlockWeights):
         """The matrices' shapes are the plan's (any number of expert slots: expert_map
         says which); the layer's calls read them by the plan's sizes."""
-        p, bf16, slots = self.layer, torch.bfloat16, weights.w_down.shape[0]
+        p, bf16 = self.layer, torch.bfloat16
         api._want(weights.w_router, "w_router", (p.E, p.d), bf16)
+        if p.mx4_act is not None:   # the layer's call checks the matrices against each other
+            for w, n, shape in ((weights.w_gate_up, "w_gate_up", (2 * p.f, p.d)),
+                                (weights.w_down, "w_down", (p.d, p.f))):
+                slots = w.codes.shape[0] if isinstance(w, api.Mx4) else 0
+                api._want_mx4(w, n, (slots,) + shape, p.out.device)
+            return
+        slots = weights.w_down.shape[0]
         api._want(weights.w_gate_up, "w_gate_up", (slots, 2 * p.f, p.d), bf16)
         api._want(weights.w_down, "w_down", (slots, p.d, p.f), bf16)
 

@@ -28,6 +28,8 @@ bits (moe_act8_save) and the backward reads those
 (moe_grouped_ffn_bwd_gather_act8): 2.06 d_ff bytes a routed row are kept instead
 of the 6 d_ff of act_save and H, which become scratch that plans run one after
 the other can share (``scratch``).
+With mx4_act=4 or 16 the expert weights are in microscaled 4 bits (api.Mx4, serving):
+moe_grouped_ffn_fwd_mx4, with activations in 4 or 16 bits, then moe_combine.
 
 All buffers are allocated once, so a pass makes no allocation and no host
 synchronisation; every step runs in the library's kernels on the current
@@ -42,16 +44,19 @@ import torch
 
 from . import api
 from ._lib import (LAEP_ACT8_BLOCK, LAEP_CALL_COUNTS, LAEP_CALL_FFN_BWD, LAEP_CALL_FFN_FWD,
-                   LAEP_CALL_ROUTE_BWD)
+                   LAEP_CALL_MX4_FFN, LAEP_CALL_ROUTE_BWD)
 
 
 class MoELayerPlan:
     def __init__(self, T: int, d_model: int, E: int, k: int, d_ff: int,
                  dtype: torch.dtype = torch.bfloat16, device="cuda", backward: bool = False,
                  save_act: Optional[bool] = None, fused_dispatch: Optional[bool] = None,
-                 act_bits: int = 16, scratch: Optional["MoELayerPlan"] = None):
+                 act_bits: int = 16, scratch: Optional["MoELayerPlan"] = None,
+                 mx4_act: Optional[int] = None):
         """``act_bits`` 8: a training plan (bf16, fused dispatch) keeps its
-        pre-activations in 8 bits.  ``scratch``: a plan of the same sizes and kind
+        pre-activations in 8 bits.  ``mx4_act`` 4 or 16: a plan without a backward (bf16,
+        fused dispatch) whose expert weights are api.Mx4, with activations in that many
+        bits.  ``scratch``: a plan of the same sizes and kind
         whose transient buffers this one uses too; their forward and backward
         passes must not overlap."""
         self.T, self.d, self.E, self.k, self.f = T, d_model, E, k, d_ff
@@ -81,7 +86,13 @@ class MoELayerPlan:
         if act_bits == 8 and not (backward and save_act and self.fused):
             raise ValueError("act_bits=8 needs a training plan with the fused dispatch (bf16)")
         self.act_bits = act_bits
-        kind = (T, d_model, E, k, d_ff, dtype, dev, backward, self.fused, act_bits)
+        if mx4_act not in (None, 4, 16):
+            raise ValueError(f"mx4_act={mx4_act} is neither 4 nor 16")
+        if mx4_act is not None and (backward or save_act or not self.fused):
+            raise ValueError("mx4_act needs a plan without a backward pass or kept "
+                             "activations, with the fused dispatch (bf16)")
+        self.mx4_act = mx4_act
+        kind = (T, d_model, E, k, d_ff, dtype, dev, backward, self.fused, act_bits, mx4_act)
         if scratch is not None and scratch.kind != kind:
             raise ValueError("scratch must be a plan of the same sizes and kind")
         self.kind = kind
@@ -95,7 +106,7 @@ class MoELayerPlan:
         # one slot per token (bf16): the combine folds into the down projection's
         # epilogue; y_perm is then written only for the backward (combine_bwd) or
         # when the caller keeps the activations (save_act)
-        self.fused_combine = k == 1 and self.fused
+        self.fused_combine = k == 1 and self.fused and mx4_act is None
         self.y_perm = (None if self.fused_combine and not (backward or save_act) else
                        torch.empty((R, d_model), dtype=dtype, device=dev))
         if scratch is not None and act_bits == 8:   # transient: decoded into 8 bits at once
@@ -118,6 +129,8 @@ class MoELayerPlan:
             self.ws_ffn = scratch.ws_ffn
         else:
             self.ws_ffn = torch.empty(
+                max(1, api.workspace_bytes(LAEP_CALL_MX4_FFN, T, k, E, d_model, d_ff))
+                if mx4_act is not None else
                 api.workspace_bytes(LAEP_CALL_FFN_FWD, R, 1, E, d_model, d_ff),
                 dtype=torch.uint8, device=dev)
         if backward:
@@ -173,7 +186,16 @@ class MoELayerPlan:
                             n_pruned=self.n_pruned)
 
     def experts_and_combine(self, x, w_gate_up, w_down, expert_map=None):
+        for w in (w_gate_up, w_down):
+            if isinstance(w, api.Mx4) != (self.mx4_act is not None):
+                raise ValueError("expert weights are Mx4 where the plan has mx4_act, and only there")
         self.x_in = x
+        if self.mx4_act is not None:
+            api.moe_grouped_ffn_fwd_mx4(x, w_gate_up, w_down, self.offsets, row_src=self.row_src,
+                                        k=self.k, act_bits=self.mx4_act, expert_map=expert_map,
+                                        ws=self.ws_ffn, y_perm=self.y_perm)
+            api.moe_combine(self.y_perm, self.topk_gate, self.dest_row, out=self.out)
+            return self.out
         if self.fused_combine:
             api.moe_grouped_ffn_fwd_gather_combine(
                 x, self.row_src, self.topk_gate, w_gate_up, w_down, self.offsets, rows=self.R,
