@@ -358,15 +358,51 @@ hipError_t launch_product(Mx4Params p, int64_t R, hipStream_t s) {
   return launch_tiles<64, ACT == ACT_MX4 ? 3 : 4, ACT, EPI>(p, R, s);
 }
 
+// Whether a product takes the 256 x 256 tiles: where experts have rows for them (at even
+// loads of 191 rows, 16 experts of d 4096, d_ff 2048 in MX4, the FFN took 118 us with them
+// and 108 without; at 1024 rows, 64 experts of 2048 and 1024, 307 and 431), and enough
+// k-steps for their pipeline.  Their offsets within a tile have 32 bits.
+bool big_tiles(int64_t R, int E, int N, int K) {
+  return R > 256 * (int64_t)E && K >= 576 && N <= 1 << 20 &&
+         mx4_scale_bytes(R, K) < (size_t)1 << 31;
+}
+
 }  // namespace
 
-size_t mx4_product_ws_bytes(int T, int k, int E, int K, int N) { return 0; }
+size_t mx4_product_ws_bytes(int T, int k, int E, int K, int N) {
+  const int64_t R = (int64_t)T * k;
+  if (!big_tiles(R, E, N, K)) return 0;
+  return mx4_big_list_bytes(R, E, N, false) + align_up(mx4_scale_bytes(R, K), 256);
+}
 
 hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32_t* row_src, int T,
                               int k, const uint8_t* w, const uint8_t* w_scale,
                               const int32_t* offsets, const int32_t* expert_map, int out_dtype,
                               int E, int N, int K, int64_t R, void* out, void* ws, hipStream_t s) {
   if (R == 0) return hipSuccess;
+  if (big_tiles((int64_t)T * k, E, N, K)) {
+    uint8_t* const list = static_cast<uint8_t*>(ws);
+    uint8_t* const routed = list + mx4_big_list_bytes((int64_t)T * k, E, N, false);
+    const bool gather = x_scale && row_src;
+    const hipError_t err =
+        launch_mx4_prepare(offsets, expert_map, E, R, 0, nullptr, N, list, x_scale,
+                           gather ? routed : nullptr, row_src, k, T, K, s);
+    if (err != hipSuccess) return err;
+    Mx4Args a = {};
+    a.A = x;
+    a.a_scale = gather ? routed : x_scale;
+    a.a_rows = gather ? R : T;
+    a.B = w;
+    a.b_scale = w_scale;
+    a.N = N;
+    a.K = K;
+    a.f32_out = out_dtype == kDtypeF32;
+    a.out = out;
+    a.row_src = row_src;
+    a.slots_k = k;
+    a.list = list;
+    return launch_mx4_big(a, s);
+  }
   Mx4Params p = {};
   p.A = x;
   p.a_scale = x_scale;
@@ -391,24 +427,30 @@ hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32
 
 namespace {
 
-// the FFN's workspace: X in MX4, then H (MX4 or bf16)
+// the FFN's workspace: X in MX4, H (MX4 or bf16), and where the products take the large
+// tiles their lists and X's scales in routed order
 struct Mx4FfnWs {
-  size_t x_scale, h, h_scale, bytes;
+  size_t x_scale, h, h_scale, list_gu, list_d, routed, bytes;
+  bool big;
 };
-Mx4FfnWs ffn_ws(int64_t T, int64_t R, int d, int f, bool mx4) {
+Mx4FfnWs ffn_ws(int64_t T, int64_t R, int E, int d, int f, bool mx4) {
   Mx4FfnWs w;
+  w.big = big_tiles(R, E, 2 * f, d) && big_tiles(R, E, d, f);
   w.x_scale = mx4 ? align_up((size_t)T * d / 2, 256) : 0;
   w.h = w.x_scale + (mx4 ? align_up(mx4_scale_bytes(T, d), 256) : 0);
   w.h_scale = w.h + align_up((size_t)R * f * 2 / (mx4 ? 4 : 1), 256);
-  w.bytes = w.h_scale + (mx4 ? align_up(mx4_scale_bytes(R, f), 256) : 0);
+  w.list_gu = w.h_scale + (mx4 ? align_up(mx4_scale_bytes(R, f), 256) : 0);
+  w.list_d = w.list_gu + (w.big ? mx4_big_list_bytes(R, E, f, true) : 0);
+  w.routed = w.list_d + (w.big ? mx4_big_list_bytes(R, E, d, false) : 0);
+  w.bytes = w.routed + (w.big && mx4 ? align_up(mx4_scale_bytes(R, d), 256) : 0);
   return w;
 }
 
 }  // namespace
 
 size_t ffn_fwd_mx4_ws_bytes(int T, int k, int E, int d, int f) {
-  const size_t a = ffn_ws(T, (int64_t)T * k, d, f, true).bytes;
-  const size_t b = ffn_ws(T, (int64_t)T * k, d, f, false).bytes;
+  const size_t a = ffn_ws(T, (int64_t)T * k, E, d, f, true).bytes;
+  const size_t b = ffn_ws(T, (int64_t)T * k, E, d, f, false).bytes;
   return a > b ? a : b;
 }
 
@@ -419,17 +461,54 @@ hipError_t launch_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int 
                               int64_t R, void* y_perm, void* act_save, void* ws, hipStream_t s) {
   if (R == 0) return hipSuccess;
   const bool mx4 = act_bits == 4;
-  const Mx4FfnWs at = ffn_ws(T, R, d, f, mx4);
+  const Mx4FfnWs at = ffn_ws(T, row_src ? (int64_t)T * k : T, E, d, f, mx4);
   uint8_t* const base = static_cast<uint8_t*>(ws);
-  Mx4Params p = {};
-  p.A = x;
-  p.a_rows = T;
   if (mx4) {
     const hipError_t err = launch_mx4_quantize(x, kDtypeBf16, 1, T, d, base, base + at.x_scale, s);
     if (err != hipSuccess) return err;
-    p.A = base;
-    p.a_scale = base + at.x_scale;
   }
+  if (at.big) {
+    const bool gather = mx4 && row_src;
+    hipError_t err = launch_mx4_prepare(
+        offsets, expert_map, E, R, f, base + at.list_gu, d, base + at.list_d, base + at.x_scale,
+        gather ? base + at.routed : nullptr, row_src, k, T, d, s);
+    if (err != hipSuccess) return err;
+    Mx4Args a = {};
+    a.A = mx4 ? base : x;
+    a.a_scale = !mx4 ? nullptr : base + (gather ? at.routed : at.x_scale);
+    a.a_rows = gather ? R : T;
+    a.B = w_gu;
+    a.b_scale = w_gu_scale;
+    a.N = 2 * f;
+    a.K = d;
+    a.f = f;
+    a.out = base + at.h;
+    a.out_scale = base + at.h_scale;
+    a.out_rows = R;
+    a.act = act_save;
+    a.row_src = row_src;
+    a.slots_k = k;
+    a.list = base + at.list_gu;
+    err = launch_mx4_big(a, s);
+    if (err != hipSuccess) return err;
+    a.A = base + at.h;
+    a.a_scale = mx4 ? base + at.h_scale : nullptr;
+    a.a_rows = R;
+    a.B = w_d;
+    a.b_scale = w_d_scale;
+    a.N = d;
+    a.K = f;
+    a.f = 0;
+    a.out = y_perm;
+    a.act = nullptr;
+    a.row_src = nullptr;
+    a.list = base + at.list_d;
+    return launch_mx4_big(a, s);
+  }
+  Mx4Params p = {};
+  p.A = mx4 ? base : x;
+  p.a_rows = T;
+  if (mx4) p.a_scale = base + at.x_scale;
   p.B = w_gu;
   p.b_scale = w_gu_scale;
   p.N = 2 * f;

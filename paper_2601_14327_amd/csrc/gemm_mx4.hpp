@@ -1,6 +1,8 @@
 // Shared pieces of the grouped MX4 products.
 #pragma once
 
+#include <type_traits>
+
 #include "gemm_common.hpp"
 #include "mx4.hpp"
 
@@ -35,6 +37,8 @@ struct Mx4Params {
   bf16_t* act;                // SwiGLU: pre-activations [R, 2f] or NULL
   const int32_t* row_src;     // gathered A rows, or NULL
   int slots_k;
+  const TileEntry* table;     // persistent products: the list of their tiles
+  const int* n_entries;
 };
 
 // One 32 x 32 x 64 step of MX4 operands; byte S of a scale dword is the lane's block's.

@@ -179,6 +179,32 @@ hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32
                               int k, const uint8_t* w, const uint8_t* w_scale,
                               const int32_t* offsets, const int32_t* expert_map, int out_dtype,
                               int E, int N, int K, int64_t R, void* out, void* ws, hipStream_t s);
+// The same products by 256 x 256 tiles (gemm_mx4_big.hip): each needs the list of its
+// tiles, and gathered MX4 activations their scales in routed order, both from
+// launch_mx4_prepare (list_gu: the list of a gate/up product as well, or NULL).
+struct Mx4Args {
+  const void* A;
+  const uint8_t* a_scale;    // NULL: A is bf16
+  int64_t a_rows;            // of a_scale
+  const uint8_t* B;
+  const uint8_t* b_scale;
+  int N, K, f;               // f: SwiGLU epilogue (N = 2f), else 0
+  bool f32_out;
+  void* out;
+  uint8_t* out_scale;
+  int64_t out_rows;
+  void* act;
+  const int32_t* row_src;
+  int slots_k;
+  void* list;
+};
+size_t mx4_big_list_bytes(int64_t R, int E, int n_cols, bool gate_up);
+hipError_t launch_mx4_prepare(const int32_t* offsets, const int32_t* expert_map, int E, int64_t R,
+                              int f, void* list_gu, int n_cols, void* list,
+                              const uint8_t* x_scale, uint8_t* routed_scale,
+                              const int32_t* row_src, int slots_k, int64_t T, int K,
+                              hipStream_t s);
+hipError_t launch_mx4_big(const Mx4Args& a, hipStream_t s);
 size_t ffn_fwd_mx4_ws_bytes(int T, int k, int E, int d, int f);
 hipError_t launch_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int k,
                               const uint8_t* w_gu, const uint8_t* w_gu_scale, const uint8_t* w_d,

@@ -143,7 +143,10 @@ SIZES = [   # T, k, E, dead, N, K
     (8, 1, 1, 0, 256, 2048), (1, 8, 16, 0, 320, 448), (16, 4, 8, 2, 192, 576),
     (70, 2, 5, 1, 448, 192), (200, 2, 3, 0, 320, 960), (129, 1, 1, 0, 128, 1088),
     (513, 1, 1, 0, 576, 512), (700, 4, 12, 3, 256, 1216), (1100, 2, 4, 0, 1088, 768),
-    (64, 2, 128, 0, 64, 704), (40, 8, 256, 100, 128, 64), (3000, 2, 7, 1, 640, 320)]
+    (64, 2, 128, 0, 64, 704), (40, 8, 256, 100, 128, 64), (3000, 2, 7, 1, 640, 320),
+    # past 256 rows an expert and 576 columns: the 256 x 256 tiles
+    (700, 1, 2, 0, 64, 576), (1400, 2, 5, 1, 704, 640), (2100, 1, 1, 0, 320, 1216),
+    (1500, 4, 9, 3, 256, 1024), (9000, 1, 30, 2, 576, 832)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -172,7 +175,8 @@ def test_grouped_product(T, k, E, dead, N, K, act, dtype):
 
 
 @pytest.mark.parametrize("act", [4, 16])
-@pytest.mark.parametrize("T,N,K", [(5, 192, 320), (300, 128, 320), (2000, 256, 448)])
+@pytest.mark.parametrize("T,N,K", [(5, 192, 320), (300, 128, 320), (2000, 256, 448),
+                                   (2000, 320, 704)])
 def test_rows_left_as_they_were_and_nans_confined(T, N, K, act):
     """Rows of experts without a slot, and behind the last expert, keep what they held; a
     row with a NaN, and an expert whose weights hold one, spoil nothing else."""
@@ -265,7 +269,9 @@ def _ffn_check(y, x, row_src, offsets, emap, gu, dn, k, act, act_save=None):
 FFN_SIZES = [   # T, k, E, dead, d, f
     (1, 1, 1, 0, 64, 64), (1, 8, 16, 0, 256, 192), (3, 2, 4, 1, 320, 64), (16, 4, 12, 3, 512, 320),
     (40, 2, 3, 0, 192, 448), (200, 2, 4, 1, 448, 256), (600, 4, 6, 0, 256, 576),
-    (1500, 1, 3, 1, 320, 192), (1000, 8, 16, 0, 128, 128), (9, 3, 200, 50, 64, 128)]
+    (1500, 1, 3, 1, 320, 192), (1000, 8, 16, 0, 128, 128), (9, 3, 200, 50, 64, 128),
+    # the 256 x 256 tiles
+    (600, 2, 3, 0, 576, 640), (1200, 1, 4, 1, 704, 576), (900, 2, 4, 0, 1024, 832)]
 
 
 @pytest.mark.parametrize("act", [4, 16])
@@ -345,10 +351,10 @@ def test_quantisation_aware_gradients():
 
 # ---- streams and graphs --------------------------------------------------------------------
 @pytest.mark.parametrize("act", [4, 16])
-@pytest.mark.parametrize("T", [2, 700])
-def test_captured_and_on_another_stream(T, act):
-    case(f"mx4 ffn in a graph, T={T} act={act}")
-    k, E, d, f = 2, 4, 256, 192
+@pytest.mark.parametrize("T,d,f", [(2, 256, 192), (700, 256, 192), (700, 576, 640)])
+def test_captured_and_on_another_stream(T, d, f, act):
+    case(f"mx4 ffn in a graph, T={T} d={d} f={f} act={act}")
+    k, E = 2, 4
     sets = [_ffn_inputs(s, T, k, E, 0, d, f) for s in (1, 2)]
     gu, dn = _mx4(sets[0][4]), _mx4(sets[0][5])
     ws = torch.empty(laep.workspace_bytes(laep.LAEP_CALL_MX4_FFN, T, k, E, d, f),
