@@ -16,7 +16,7 @@ import torch
 from ._lib import (LAEP_ACT8_BLOCK, LAEP_BF16, LAEP_CALL_BALANCE, LAEP_CALL_COUNTS,
                    LAEP_CALL_FFN_BWD, LAEP_CALL_FFN_FWD, LAEP_CALL_LAYER_NORM_BWD,
                    LAEP_CALL_MX4_FFN, LAEP_CALL_MX4_PRODUCT, LAEP_CALL_ROUTE_BWD, LAEP_F32,
-                   LAEP_MX4_BLOCK, LAEP_MX4_GROUP, LaepError, check, lib)
+                   LAEP_MX4_GROUP, LaepError, check, lib)
 
 _DT = {torch.float32: LAEP_F32, torch.bfloat16: LAEP_BF16}
 
@@ -811,48 +811,65 @@ class Mx4(NamedTuple):
     scale: torch.Tensor
 
 
-def _mx4_scale_shape(R: int, C: int):
-    return (-(-C // LAEP_MX4_GROUP), R, LAEP_MX4_GROUP // LAEP_MX4_BLOCK)
+def _need(t, name: str, shape, dtype, device):
+    """A given tensor of this shape, dtype and device.  (The checks of a small call cost
+    as much as its kernels: one pass over the attributes when all is well.)"""
+    if not (t.shape == shape and t.dtype is dtype and t.get_device() == device.index
+            and t.is_contiguous()):
+        _want(t, name, shape, dtype)
+        raise ValueError(f"{name} is on {t.device}, not {device}")
 
 
-def _want_mx4(w, name: str, shape, device):
-    """A given Mx4 of this matrix shape, on this device."""
+def _need_out(t, name: str, shape, dtype, device):
+    """The given output buffer, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _need(t, name, shape, dtype, device)
+    return t
+
+
+def _need_ws(ws, device, which, *sizes):
+    """The given workspace (its size is the C call's to check) or a new one."""
+    if ws is None:
+        return _given_ws(None, device, which, *sizes)
+    if ws.get_device() != device.index or not ws.is_contiguous():
+        _dev(ws, "ws")
+        raise ValueError(f"ws is on {ws.device}, not {device}")
+    return ws
+
+
+def _need_mx4(w, name: str, lead, R: int, C: int, device):
+    """A given Mx4 [*lead, R, C]."""
     if not isinstance(w, Mx4):
         raise ValueError(f"{name} must be an Mx4 (moe_mx4_quantize's codes and scale)")
-    lead = tuple(shape[:-2])
-    _want(w.codes, f"{name}.codes", lead + (shape[-2], shape[-1] // 2), torch.uint8)
-    _want(w.scale, f"{name}.scale", lead + _mx4_scale_shape(*shape[-2:]), torch.uint8)
-    _same_device(device, **{f"{name}.codes": w.codes, f"{name}.scale": w.scale})
-
-
-def _same_device(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not {device}")
+    _need(w[0], f"{name}.codes", lead + (R, C // 2), torch.uint8, device)
+    _need(w[1], f"{name}.scale", lead + (-(-C // LAEP_MX4_GROUP), R, 8), torch.uint8, device)
 
 
 def _on_device(device, fn, *args):
-    """check(fn(*args)) with the tensors' device current: the C calls launch there."""
-    if torch.cuda.current_device() == device.index:
-        check(fn(*args))
+    """check(fn(*args, stream)) with the tensors' device current: the C calls launch there."""
+    index = device.index
+    if torch._C._cuda_getDevice() == index:
+        check(fn(*args, torch._C._cuda_getCurrentRawStream(index)))
     else:
         with torch.cuda.device(device):
-            check(fn(*args))
+            check(fn(*args, torch._C._cuda_getCurrentRawStream(index)))
 
 
 def moe_mx4_quantize(src: torch.Tensor, *, codes=None, scale=None) -> Mx4:
     """The matrices src [..., R, C] (bf16 or float32, C a multiple of 32) in
     microscaled 4 bits: every 32 columns of a row share a power-of-two scale."""
     _dev(src, "src")
-    if src.dim() < 2:
+    shape = tuple(src.shape)
+    if len(shape) < 2:
         raise ValueError("src must have rows and columns")
-    lead, (R, C) = tuple(src.shape[:-2]), src.shape[-2:]
+    lead, R, C = shape[:-2], shape[-2], shape[-1]
+    dev = src.device
     code = _dtype_code(src)
-    codes = _out(codes, "codes", lead + (R, C // 2), torch.uint8, src.device)
-    scale = _out(scale, "scale", lead + _mx4_scale_shape(R, C), torch.uint8, src.device)
-    _same_device(src.device, codes=codes, scale=scale)
-    _on_device(src.device, lib().moe_mx4_quantize, _ptr(src), code, math.prod(lead), R, C,
-               _ptr(codes), _ptr(scale), _stream(src.device))
+    codes = _need_out(codes, "codes", lead + (R, C // 2), torch.uint8, dev)
+    scale = _need_out(scale, "scale", lead + (-(-C // LAEP_MX4_GROUP), R, 8), torch.uint8, dev)
+    _on_device(dev, lib().moe_mx4_quantize, src.data_ptr(), code, math.prod(lead), R, C,
+               codes.data_ptr(), scale.data_ptr())
     return Mx4(codes, scale)
 
 
@@ -860,18 +877,17 @@ def moe_mx4_dequantize(codes: torch.Tensor, scale: torch.Tensor,
                        dtype: torch.dtype = torch.bfloat16, *, out=None):
     """The values [..., R, C] that codes and scale stand for, in dtype (exact)."""
     _dev(codes, "codes")
-    if codes.dim() < 2:
+    shape = tuple(codes.shape)
+    if len(shape) < 2:
         raise ValueError("codes must have rows and columns")
-    lead, R, C = tuple(codes.shape[:-2]), codes.shape[-2], 2 * codes.shape[-1]
+    lead, R, C = shape[:-2], shape[-2], 2 * shape[-1]
     dev = codes.device
     if dtype not in _DT:
         raise LaepError(2, f"unsupported dtype {dtype}")
-    _want(codes, "codes", codes.shape, torch.uint8)
-    _want(scale, "scale", lead + _mx4_scale_shape(R, C), torch.uint8)
-    out = _out(out, "out", lead + (R, C), dtype, dev)
-    _same_device(dev, scale=scale, out=out)
-    _on_device(dev, lib().moe_mx4_dequantize, _ptr(codes), _ptr(scale), _DT[dtype],
-               math.prod(lead), R, C, _ptr(out), _stream(dev))
+    _need_mx4(Mx4(codes, scale), "Mx4", lead, R, C, dev)
+    out = _need_out(out, "out", lead + (R, C), dtype, dev)
+    _on_device(dev, lib().moe_mx4_dequantize, codes.data_ptr(), scale.data_ptr(), _DT[dtype],
+               math.prod(lead), R, C, out.data_ptr())
     return out
 
 
@@ -879,15 +895,17 @@ def _mx4_routing(dev, T: int, k: int, offsets, row_src, expert_map, slots: int):
     """Checks of the routing's tensors.  Returns (E, R, k as the C calls take it)."""
     if offsets.dim() != 1 or offsets.numel() < 2:
         raise ValueError("offsets must be an int32 tensor [E + 1]")
-    E = offsets.shape[0] - 1
-    _want(offsets, "offsets", (E + 1,), torch.int32)
-    if row_src is not None:
-        _want(row_src, "row_src", (row_src.numel(),), torch.int32)
-    _want(expert_map, "expert_map", (E,), torch.int32)
-    if expert_map is None and slots != E:
+    E = offsets.numel() - 1
+    _need(offsets, "offsets", (E + 1,), torch.int32, dev)
+    if expert_map is not None:
+        _need(expert_map, "expert_map", (E,), torch.int32, dev)
+    elif slots != E:
         raise ValueError(f"{slots} weight slots for {E} experts need an expert_map")
-    _same_device(dev, offsets=offsets, row_src=row_src, expert_map=expert_map)
-    return E, (T if row_src is None else row_src.numel()), (1 if row_src is None else k)
+    if row_src is None:
+        return E, T, 1
+    R = row_src.numel()
+    _need(row_src, "row_src", (R,), torch.int32, dev)
+    return E, R, k
 
 
 def moe_mx4_grouped_product(x, w: Mx4, offsets: torch.Tensor, *, row_src=None, k: int = 1,
@@ -898,28 +916,28 @@ def moe_mx4_grouped_product(x, w: Mx4, offsets: torch.Tensor, *, row_src=None, k
     K] (N, K multiples of 64); without row_src x's rows are already in the experts'
     order.  Rows of experts with a negative expert_map entry are left as they were."""
     mx4 = isinstance(x, Mx4)
-    rows = x.codes if mx4 else x
+    rows = x[0] if mx4 else x
     _dev(rows, "x")
-    if rows.dim() != 2 or not isinstance(w, Mx4) or w.codes.dim() != 3:
+    if rows.dim() != 2 or not isinstance(w, Mx4) or w[0].dim() != 3:
         raise ValueError("x must be a matrix [T, K], w an Mx4 of [slots, N, K]")
     dev = rows.device
-    T, K = rows.shape[0], rows.shape[1] * (2 if mx4 else 1)
-    slots, N = w.codes.shape[:2]
-    _want_mx4(w, "w", (slots, N, K), dev)
+    T, K = rows.shape
+    slots, N, _ = w[0].shape
     if mx4:
-        _want_mx4(x, "x", (T, K), dev)
+        K *= 2
+        _need_mx4(x, "x", (), T, K, dev)
     else:
-        _want(x, "x", (T, K), torch.bfloat16)
+        _need(x, "x", (T, K), torch.bfloat16, dev)
+    _need_mx4(w, "w", (slots,), N, K, dev)
     if dtype not in _DT:
         raise LaepError(2, f"unsupported dtype {dtype}")
     E, R, k = _mx4_routing(dev, T, k, offsets, row_src, expert_map, slots)
-    out = _out(out, "out", (R, N), dtype, dev)
-    ws = _given_ws(ws, dev, LAEP_CALL_MX4_PRODUCT, T, k, E, K, N)
-    _same_device(dev, out=out, ws=ws)
-    _on_device(dev, lib().moe_mx4_grouped_product, _ptr(rows), _ptr(x.scale) if mx4 else None,
-               _ptr(row_src), T, k, _ptr(w.codes), _ptr(w.scale), _ptr(offsets),
-               _ptr(expert_map), _DT[dtype], E, N, K, R, _ptr(out), _ptr(ws),
-               ws.numel() * ws.element_size(), _stream(dev))
+    out = _need_out(out, "out", (R, N), dtype, dev)
+    ws = _need_ws(ws, dev, LAEP_CALL_MX4_PRODUCT, T, k, E, K, N)
+    _on_device(dev, lib().moe_mx4_grouped_product, rows.data_ptr(),
+               x[1].data_ptr() if mx4 else None, _ptr(row_src), T, k, w[0].data_ptr(),
+               w[1].data_ptr(), offsets.data_ptr(), _ptr(expert_map), _DT[dtype], E, N, K, R,
+               out.data_ptr(), ws.data_ptr(), ws.nbytes)
     return out
 
 
@@ -934,26 +952,25 @@ def moe_grouped_ffn_fwd_mx4(x: torch.Tensor, w_gate_up: Mx4, w_down: Mx4,
     moe_grouped_ffn_bwd_gather at moe_mx4_dequantize of the weights.  Returns (y_perm
     [R, d], act_save [R, 2f] or None)."""
     _dev(x, "x")
-    if x.dim() != 2 or any(not isinstance(w, Mx4) or w.codes.dim() != 3
-                           for w in (w_gate_up, w_down)):
+    if x.dim() != 2 or not isinstance(w_gate_up, Mx4) or not isinstance(w_down, Mx4) or \
+            w_down[0].dim() != 3:
         raise ValueError("x must be a matrix [T, d], the weights Mx4 of [slots, ., .]")
     dev = x.device
     T, d = x.shape
-    slots, f = w_down.codes.shape[0], 2 * w_down.codes.shape[2]
-    _want(x, "x", (T, d), torch.bfloat16)
-    _want_mx4(w_gate_up, "w_gate_up", (slots, 2 * f, d), dev)
-    _want_mx4(w_down, "w_down", (slots, d, f), dev)
+    slots, _, f = w_down[0].shape
+    f *= 2
+    _need(x, "x", (T, d), torch.bfloat16, dev)
+    _need_mx4(w_gate_up, "w_gate_up", (slots,), 2 * f, d, dev)
+    _need_mx4(w_down, "w_down", (slots,), d, f, dev)
     E, R, k = _mx4_routing(dev, T, k, offsets, row_src, expert_map, slots)
-    y_perm = _out(y_perm, "y_perm", (R, d), torch.bfloat16, dev)
+    y_perm = _need_out(y_perm, "y_perm", (R, d), torch.bfloat16, dev)
     if save_act or act_save is not None:
-        act_save = _out(act_save, "act_save", (R, 2 * f), torch.bfloat16, dev)
-    ws = _given_ws(ws, dev, LAEP_CALL_MX4_FFN, T, k, E, d, f)
-    _same_device(dev, y_perm=y_perm, act_save=act_save, ws=ws)
-    _on_device(dev, lib().moe_grouped_ffn_fwd_mx4, _ptr(x), _ptr(row_src), T, k,
-               _ptr(w_gate_up.codes), _ptr(w_gate_up.scale), _ptr(w_down.codes),
-               _ptr(w_down.scale), _ptr(offsets), _ptr(expert_map), int(act_bits), E, d, f, R,
-               _ptr(y_perm), _ptr(act_save), _ptr(ws), ws.numel() * ws.element_size(),
-               _stream(dev))
+        act_save = _need_out(act_save, "act_save", (R, 2 * f), torch.bfloat16, dev)
+    ws = _need_ws(ws, dev, LAEP_CALL_MX4_FFN, T, k, E, d, f)
+    _on_device(dev, lib().moe_grouped_ffn_fwd_mx4, x.data_ptr(), _ptr(row_src), T, k,
+               w_gate_up[0].data_ptr(), w_gate_up[1].data_ptr(), w_down[0].data_ptr(),
+               w_down[1].data_ptr(), offsets.data_ptr(), _ptr(expert_map), int(act_bits), E, d, f,
+               R, y_perm.data_ptr(), _ptr(act_save), ws.data_ptr(), ws.nbytes)
     return y_perm, act_save
 
 

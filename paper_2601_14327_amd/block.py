@@ -96,7 +96,7 @@ class MoEBlockPlan:
             for w, n, shape in ((weights.w_gate_up, "w_gate_up", (2 * p.f, p.d)),
                                 (weights.w_down, "w_down", (p.d, p.f))):
                 slots = w.codes.shape[0] if isinstance(w, api.Mx4) else 0
-                api._want_mx4(w, n, (slots,) + shape, p.out.device)
+                api._need_mx4(w, n, (slots,), *shape, p.out.device)
             return
         slots = weights.w_down.shape[0]
         api._want(weights.w_gate_up, "w_gate_up", (slots, 2 * p.f, p.d), bf16)

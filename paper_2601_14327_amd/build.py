@@ -20,7 +20,7 @@ LIB = os.path.join(HERE, "liblaep_moe.so")
 HIP_SOURCES = ["route.hip", "route_bwd.hip", "counts.hip", "prune.hip", "compact.hip", "rowops.hip",
                "gemm_bf16.hip", "gemm_small.hip", "gemm_bwd.hip", "gemm_f32.hip", "calib.hip", "noalloc.hip",
                "norm.hip", "balance.hip", "act8.hip", "mx4.hip", "gemm_mx4.hip",
-               "gemm_mx4_big.hip"]
+               "gemm_mx4_big.hip", "gemm_mx4_few.hip"]
 HIP_HOST_SOURCES = ["api.cpp", "streams.cpp"]   # host code that calls the HIP runtime
 CXX_SOURCES = ["rearrange.cpp"]         # plain host C++
 

@@ -991,7 +991,7 @@ int moe_mx4_grouped_product(const void* x, const uint8_t* x_scale, const int32_t
   if ((rc = check_mx4_act(name, T, K, x_scale != nullptr))) return rc;
   REQUIRE(offsets, LAEP_ERR_INVALID_ARG, "%s: offsets must be non-null", name);
   if (R == 0) return ok();
-  const size_t need = laep::mx4_product_ws_bytes(T, k, E, K, N);
+  const size_t need = laep::mx4_product_ws_bytes(T, row_src ? k : 1, E, K, N);
   REQUIRE(x && w && w_scale && out && (ws || need == 0), LAEP_ERR_INVALID_ARG,
           "%s: x, w, w_scale, out and ws must be non-null", name);
   REQUIRE(aligned16(x) && aligned16(x_scale) && aligned16(w) && aligned16(w_scale) &&

@@ -350,28 +350,55 @@ hipError_t launch_tiles(const Mx4Params& p, int64_t R, hipStream_t s) {
   return hipGetLastError();
 }
 
-// one product with its epilogue, by the kernel that suits its sizes
 template <int ACT, int EPI>
-hipError_t launch_product(Mx4Params p, int64_t R, hipStream_t s) {
+hipError_t launch_middle(Mx4Params p, int64_t R, hipStream_t s) {
   p.n_tiles_n = EPI == MX4_GU ? p.f / 64 : ceil_div(p.N, 128);
   if (R > 64 * (int64_t)p.E) return launch_tiles<128, 2, ACT, EPI>(p, R, s);
   return launch_tiles<64, ACT == ACT_MX4 ? 3 : 4, ACT, EPI>(p, R, s);
 }
 
-// Whether a product takes the 256 x 256 tiles: where experts have rows for them (at even
-// loads of 191 rows, 16 experts of d 4096, d_ff 2048 in MX4, the FFN took 118 us with them
-// and 108 without; at 1024 rows, 64 experts of 2048 and 1024, 307 and 431), and enough
-// k-steps for their pipeline.  Their offsets within a tile have 32 bits.
-bool big_tiles(int64_t R, int E, int N, int K) {
-  return R > 256 * (int64_t)E && K >= 576 && N <= 1 << 20 &&
-         mx4_scale_bytes(R, K) < (size_t)1 << 31;
+// The tiles of a product [R, K] x [N, K]^T over E experts: 32 x 64 for few rows an expert
+// (FEW), 64 or 128 x 128 (MIDDLE), or the persistent 256 x 256 (BIG).
+enum Tiles { FEW, MIDDLE, BIG };
+
+// BIG: where experts have rows for them (at even loads of 191 rows, 16 experts of d 4096,
+// d_ff 2048 in MX4, the FFN took 118 us with them and 108 without; at 1024 rows, 64 experts
+// of 2048 and 1024, 307 and 431), and enough k-steps for their pipeline.  Their offsets
+// within a tile have 32 bits.
+Tiles tiles_of(int64_t R, int E, int N, int K) {
+  if (R <= 16 * (int64_t)E) return FEW;
+  if (R > 256 * (int64_t)E && K >= 576 && N <= 1 << 20 && mx4_scale_bytes(R, K) < (size_t)1 << 31)
+    return BIG;
+  return MIDDLE;
+}
+
+// one product with its epilogue, by the kernel that suits its sizes (R: the rows that the
+// workspace was sized for, at least the call's)
+hipError_t launch_product(const Mx4Args& a, bool round, const int32_t* offsets,
+                          const int32_t* expert_map, int E, int64_t R, int64_t R_call,
+                          hipStream_t s) {
+  const Tiles kind = tiles_of(R, E, a.N, a.K);
+  if (kind == FEW) return launch_mx4_few(a, round, offsets, expert_map, E, R_call, s);
+  if (kind == BIG) return launch_mx4_big(a, s);
+  Mx4Params p = mx4_params(a);
+  p.offsets = offsets;
+  p.expert_map = expert_map;
+  p.E = E;
+  if (a.a_scale) {
+    if (a.f) return launch_middle<ACT_MX4, MX4_GU>(p, R_call, s);
+    return a.f32_out ? launch_middle<ACT_MX4, MX4_STORE_F32>(p, R_call, s)
+                     : launch_middle<ACT_MX4, MX4_STORE>(p, R_call, s);
+  }
+  if (a.f) return launch_middle<ACT_BF16, MX4_GU>(p, R_call, s);
+  return a.f32_out ? launch_middle<ACT_BF16, MX4_STORE_F32>(p, R_call, s)
+                   : launch_middle<ACT_BF16, MX4_STORE>(p, R_call, s);
 }
 
 }  // namespace
 
 size_t mx4_product_ws_bytes(int T, int k, int E, int K, int N) {
   const int64_t R = (int64_t)T * k;
-  if (!big_tiles(R, E, N, K)) return 0;
+  if (tiles_of(R, E, N, K) != BIG) return 0;
   return mx4_big_list_bytes(R, E, N, false) + align_up(mx4_scale_bytes(R, K), 256);
 }
 
@@ -380,49 +407,35 @@ hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32
                               const int32_t* offsets, const int32_t* expert_map, int out_dtype,
                               int E, int N, int K, int64_t R, void* out, void* ws, hipStream_t s) {
   if (R == 0) return hipSuccess;
-  if (big_tiles((int64_t)T * k, E, N, K)) {
+  const int64_t R_ws = row_src ? (int64_t)T * k : T;
+  Mx4Args a = {};
+  a.A = x;
+  a.a_scale = x_scale;
+  a.a_rows = T;
+  a.B = w;
+  a.b_scale = w_scale;
+  a.N = N;
+  a.K = K;
+  a.f32_out = out_dtype == kDtypeF32;
+  a.out = out;
+  a.out_rows = R;
+  a.row_src = row_src;
+  a.slots_k = k;
+  if (tiles_of(R_ws, E, N, K) == BIG) {
     uint8_t* const list = static_cast<uint8_t*>(ws);
-    uint8_t* const routed = list + mx4_big_list_bytes((int64_t)T * k, E, N, false);
+    uint8_t* const routed = list + mx4_big_list_bytes(R_ws, E, N, false);
     const bool gather = x_scale && row_src;
     const hipError_t err =
         launch_mx4_prepare(offsets, expert_map, E, R, 0, nullptr, N, list, x_scale,
                            gather ? routed : nullptr, row_src, k, T, K, s);
     if (err != hipSuccess) return err;
-    Mx4Args a = {};
-    a.A = x;
-    a.a_scale = gather ? routed : x_scale;
-    a.a_rows = gather ? R : T;
-    a.B = w;
-    a.b_scale = w_scale;
-    a.N = N;
-    a.K = K;
-    a.f32_out = out_dtype == kDtypeF32;
-    a.out = out;
-    a.row_src = row_src;
-    a.slots_k = k;
+    if (gather) {
+      a.a_scale = routed;
+      a.a_rows = R;
+    }
     a.list = list;
-    return launch_mx4_big(a, s);
   }
-  Mx4Params p = {};
-  p.A = x;
-  p.a_scale = x_scale;
-  p.a_rows = T;
-  p.B = w;
-  p.b_scale = w_scale;
-  p.N = N;
-  p.K = K;
-  p.offsets = offsets;
-  p.expert_map = expert_map;
-  p.E = E;
-  p.out = out;
-  p.out_rows = R;
-  p.row_src = row_src;
-  p.slots_k = k;
-  if (x_scale)
-    return out_dtype == kDtypeBf16 ? launch_product<ACT_MX4, MX4_STORE>(p, R, s)
-                                   : launch_product<ACT_MX4, MX4_STORE_F32>(p, R, s);
-  return out_dtype == kDtypeBf16 ? launch_product<ACT_BF16, MX4_STORE>(p, R, s)
-                                 : launch_product<ACT_BF16, MX4_STORE_F32>(p, R, s);
+  return launch_product(a, false, offsets, expert_map, E, R_ws, R, s);
 }
 
 namespace {
@@ -431,18 +444,20 @@ namespace {
 // tiles their lists and X's scales in routed order
 struct Mx4FfnWs {
   size_t x_scale, h, h_scale, list_gu, list_d, routed, bytes;
-  bool big;
+  Tiles gu, down;
 };
 Mx4FfnWs ffn_ws(int64_t T, int64_t R, int E, int d, int f, bool mx4) {
   Mx4FfnWs w;
-  w.big = big_tiles(R, E, 2 * f, d) && big_tiles(R, E, d, f);
-  w.x_scale = mx4 ? align_up((size_t)T * d / 2, 256) : 0;
-  w.h = w.x_scale + (mx4 ? align_up(mx4_scale_bytes(T, d), 256) : 0);
+  w.gu = tiles_of(R, E, 2 * f, d);
+  w.down = tiles_of(R, E, d, f);
+  const bool x = mx4 && w.gu != FEW, big = w.gu == BIG || w.down == BIG;
+  w.x_scale = x ? align_up((size_t)T * d / 2, 256) : 0;
+  w.h = w.x_scale + (x ? align_up(mx4_scale_bytes(T, d), 256) : 0);
   w.h_scale = w.h + align_up((size_t)R * f * 2 / (mx4 ? 4 : 1), 256);
   w.list_gu = w.h_scale + (mx4 ? align_up(mx4_scale_bytes(R, f), 256) : 0);
-  w.list_d = w.list_gu + (w.big ? mx4_big_list_bytes(R, E, f, true) : 0);
-  w.routed = w.list_d + (w.big ? mx4_big_list_bytes(R, E, d, false) : 0);
-  w.bytes = w.routed + (w.big && mx4 ? align_up(mx4_scale_bytes(R, d), 256) : 0);
+  w.list_d = w.list_gu + (big ? mx4_big_list_bytes(R, E, f, true) : 0);
+  w.routed = w.list_d + (big ? mx4_big_list_bytes(R, E, d, false) : 0);
+  w.bytes = w.routed + (w.gu == BIG && mx4 ? align_up(mx4_scale_bytes(R, d), 256) : 0);
   return w;
 }
 
@@ -461,83 +476,56 @@ hipError_t launch_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int 
                               int64_t R, void* y_perm, void* act_save, void* ws, hipStream_t s) {
   if (R == 0) return hipSuccess;
   const bool mx4 = act_bits == 4;
-  const Mx4FfnWs at = ffn_ws(T, row_src ? (int64_t)T * k : T, E, d, f, mx4);
+  const int64_t R_ws = row_src ? (int64_t)T * k : T;
+  const Mx4FfnWs at = ffn_ws(T, R_ws, E, d, f, mx4);
   uint8_t* const base = static_cast<uint8_t*>(ws);
-  if (mx4) {
-    const hipError_t err = launch_mx4_quantize(x, kDtypeBf16, 1, T, d, base, base + at.x_scale, s);
+  Mx4Args a = {};
+  a.A = x;
+  a.a_rows = T;
+  hipError_t err = hipSuccess;
+  if (mx4 && at.gu != FEW) {
+    err = launch_mx4_quantize(x, kDtypeBf16, 1, T, d, base, base + at.x_scale, s);
     if (err != hipSuccess) return err;
+    a.A = base;
+    a.a_scale = base + at.x_scale;
   }
-  if (at.big) {
-    const bool gather = mx4 && row_src;
-    hipError_t err = launch_mx4_prepare(
-        offsets, expert_map, E, R, f, base + at.list_gu, d, base + at.list_d, base + at.x_scale,
-        gather ? base + at.routed : nullptr, row_src, k, T, d, s);
+  if (at.gu == BIG || at.down == BIG) {
+    const bool gather = at.gu == BIG && mx4 && row_src;
+    err = launch_mx4_prepare(offsets, expert_map, E, R, f, base + at.list_gu, d, base + at.list_d,
+                             a.a_scale, gather ? base + at.routed : nullptr, row_src, k, T, d, s);
     if (err != hipSuccess) return err;
-    Mx4Args a = {};
-    a.A = mx4 ? base : x;
-    a.a_scale = !mx4 ? nullptr : base + (gather ? at.routed : at.x_scale);
-    a.a_rows = gather ? R : T;
-    a.B = w_gu;
-    a.b_scale = w_gu_scale;
-    a.N = 2 * f;
-    a.K = d;
-    a.f = f;
-    a.out = base + at.h;
-    a.out_scale = base + at.h_scale;
-    a.out_rows = R;
-    a.act = act_save;
-    a.row_src = row_src;
-    a.slots_k = k;
-    a.list = base + at.list_gu;
-    err = launch_mx4_big(a, s);
-    if (err != hipSuccess) return err;
-    a.A = base + at.h;
-    a.a_scale = mx4 ? base + at.h_scale : nullptr;
-    a.a_rows = R;
-    a.B = w_d;
-    a.b_scale = w_d_scale;
-    a.N = d;
-    a.K = f;
-    a.f = 0;
-    a.out = y_perm;
-    a.act = nullptr;
-    a.row_src = nullptr;
-    a.list = base + at.list_d;
-    return launch_mx4_big(a, s);
+    if (gather) {
+      a.a_scale = base + at.routed;
+      a.a_rows = R;
+    }
   }
-  Mx4Params p = {};
-  p.A = mx4 ? base : x;
-  p.a_rows = T;
-  if (mx4) p.a_scale = base + at.x_scale;
-  p.B = w_gu;
-  p.b_scale = w_gu_scale;
-  p.N = 2 * f;
-  p.K = d;
-  p.f = f;
-  p.offsets = offsets;
-  p.expert_map = expert_map;
-  p.E = E;
-  p.out = base + at.h;
-  p.out_scale = base + at.h_scale;
-  p.out_rows = R;
-  p.act = static_cast<bf16_t*>(act_save);
-  p.row_src = row_src;
-  p.slots_k = k;
-  hipError_t err = mx4 ? launch_product<ACT_MX4, MX4_GU>(p, R, s)
-                       : launch_product<ACT_BF16, MX4_GU>(p, R, s);
+  a.B = w_gu;
+  a.b_scale = w_gu_scale;
+  a.N = 2 * f;
+  a.K = d;
+  a.f = f;
+  a.out = base + at.h;
+  a.out_scale = base + at.h_scale;
+  a.out_rows = R;
+  a.act = act_save;
+  a.row_src = row_src;
+  a.slots_k = k;
+  a.list = base + at.list_gu;
+  err = launch_product(a, mx4, offsets, expert_map, E, R_ws, R, s);
   if (err != hipSuccess) return err;
-  p.A = p.out;
-  p.a_scale = p.out_scale;
-  p.a_rows = R;
-  p.B = w_d;
-  p.b_scale = w_d_scale;
-  p.N = d;
-  p.K = f;
-  p.out = y_perm;
-  p.act = nullptr;
-  p.row_src = nullptr;
-  return mx4 ? launch_product<ACT_MX4, MX4_STORE>(p, R, s)
-             : launch_product<ACT_BF16, MX4_STORE>(p, R, s);
+  a.A = a.out;
+  a.a_scale = mx4 ? a.out_scale : nullptr;
+  a.a_rows = R;
+  a.B = w_d;
+  a.b_scale = w_d_scale;
+  a.N = d;
+  a.K = f;
+  a.f = 0;
+  a.out = y_perm;
+  a.act = nullptr;
+  a.row_src = nullptr;
+  a.list = base + at.list_d;
+  return launch_product(a, false, offsets, expert_map, E, R_ws, R, s);
 }
 
 }  // namespace laep

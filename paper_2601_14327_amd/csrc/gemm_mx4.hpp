@@ -41,6 +41,25 @@ struct Mx4Params {
   const int* n_entries;
 };
 
+inline Mx4Params mx4_params(const Mx4Args& a) {
+  Mx4Params p = {};
+  p.A = a.A;
+  p.a_scale = a.a_scale;
+  p.a_rows = a.a_rows;
+  p.B = a.B;
+  p.b_scale = a.b_scale;
+  p.N = a.N;
+  p.K = a.K;
+  p.f = a.f;
+  p.out = a.out;
+  p.out_scale = a.out_scale;
+  p.out_rows = a.out_rows;
+  p.act = static_cast<bf16_t*>(a.act);
+  p.row_src = a.row_src;
+  p.slots_k = a.slots_k;
+  return p;
+}
+
 // One 32 x 32 x 64 step of MX4 operands; byte S of a scale dword is the lane's block's.
 template <int S>
 __device__ __forceinline__ f32x16_t mfma_mx4(const u32x4_t& a, const u32x4_t& b, uint32_t sa,
@@ -66,6 +85,12 @@ __device__ __forceinline__ void dma_scales(char* dst, __amdgpu_buffer_rsrc_t rsr
                                            int soff, int wave) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_t*)(dst + wave * 256), 4, voff, soff, 0,
                                            0);
+}
+
+// values the compiler knows nothing about from here on
+template <typename T>
+__device__ __forceinline__ void opaque(T& a, T& b) {
+  asm volatile("" : "+v"(a), "+v"(b));
 }
 
 // H of one row's 32 columns in MX4: half the columns are in lane l, half in lane l ^ 32

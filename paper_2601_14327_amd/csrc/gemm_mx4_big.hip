@@ -26,12 +26,6 @@ struct BigTile {
   int row0, rows, phys, nt;
 };
 
-// values the compiler knows nothing about from here on
-template <typename T>
-__device__ __forceinline__ void opaque(T& a, T& b) {
-  asm volatile("" : "+v"(a), "+v"(b));
-}
-
 // H in MX4 needs a row's columns in one lane (its blocks' largest magnitudes); the other
 // outputs take the columns along the lanes, so that a store covers whole lines of a row.
 template <int ACT, int EPI>
@@ -620,21 +614,7 @@ hipError_t launch_mx4_prepare(const int32_t* offsets, const int32_t* expert_map,
 }
 
 hipError_t launch_mx4_big(const Mx4Args& a, hipStream_t s) {
-  Mx4Params p = {};
-  p.A = a.A;
-  p.a_scale = a.a_scale;
-  p.a_rows = a.a_rows;
-  p.B = a.B;
-  p.b_scale = a.b_scale;
-  p.N = a.N;
-  p.K = a.K;
-  p.f = a.f;
-  p.out = a.out;
-  p.out_scale = a.out_scale;
-  p.out_rows = a.out_rows;
-  p.act = static_cast<bf16_t*>(a.act);
-  p.row_src = a.row_src;
-  p.slots_k = a.slots_k;
+  Mx4Params p = mx4_params(a);
   const TableWs t = carve_table(a.list, 0);
   p.table = t.table;
   p.n_entries = t.n_entries;

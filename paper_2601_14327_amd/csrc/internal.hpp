@@ -205,6 +205,10 @@ hipError_t launch_mx4_prepare(const int32_t* offsets, const int32_t* expert_map,
                               const int32_t* row_src, int slots_k, int64_t T, int K,
                               hipStream_t s);
 hipError_t launch_mx4_big(const Mx4Args& a, hipStream_t s);
+// And by 32 x 64 tiles for few rows (gemm_mx4_few.hip; no list).  round: the bf16
+// activations of a gate/up product become MX4 as they are read, and H is MX4.
+hipError_t launch_mx4_few(const Mx4Args& a, bool round, const int32_t* offsets,
+                          const int32_t* expert_map, int E, int64_t R, hipStream_t s);
 size_t ffn_fwd_mx4_ws_bytes(int T, int k, int E, int d, int f);
 hipError_t launch_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int k,
                               const uint8_t* w_gu, const uint8_t* w_gu_scale, const uint8_t* w_d,

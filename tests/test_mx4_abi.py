@@ -120,9 +120,9 @@ def test_host_tensors_and_other_layouts_are_refused():
     with pytest.raises(ValueError, match="x must be a device tensor"):
         laep.moe_grouped_ffn_fwd_mx4(x, w, w, off)
     with pytest.raises(ValueError, match="must be an Mx4"):
-        api._want_mx4(torch.zeros(1, 64, 32, dtype=u8), "w", (1, 64, 64), x.device)
+        api._need_mx4(torch.zeros(1, 64, 32, dtype=u8), "w", (1,), 64, 64, x.device)
     with pytest.raises(ValueError, match=r"w.codes must be torch.uint8 \(1, 64, 64\)"):
-        api._want_mx4(w, "w", (1, 64, 128), x.device)
+        api._need_mx4(w, "w", (1,), 64, 128, x.device)
 
 
 @pytest.mark.gpu
