@@ -351,55 +351,96 @@ hipError_t launch_tiles(const Mx4Params& p, int64_t R, hipStream_t s) {
 }
 
 template <int ACT, int EPI>
-hipError_t launch_middle(Mx4Params p, int64_t R, hipStream_t s) {
+hipError_t launch_middle(Mx4Params p, int bm, int64_t R, hipStream_t s) {
   p.n_tiles_n = EPI == MX4_GU ? p.f / 64 : ceil_div(p.N, 128);
-  if (R > 64 * (int64_t)p.E) return launch_tiles<128, 2, ACT, EPI>(p, R, s);
+  if (bm == 128) return launch_tiles<128, 2, ACT, EPI>(p, R, s);
   return launch_tiles<64, ACT == ACT_MX4 ? 3 : 4, ACT, EPI>(p, R, s);
 }
 
-// The tiles of a product [R, K] x [N, K]^T over E experts: 32 x 64 for few rows an expert
-// (FEW), 64 or 128 x 128 (MIDDLE), or the persistent 256 x 256 (BIG).
-enum Tiles { FEW, MIDDLE, BIG };
+// The tiles of a product over E experts: 32 x 64 for few rows an expert (FEW), 64 or 128 x
+// 128, or the persistent 128 or 256 x 256 (BIG).
+enum Tiles { FEW, MID64, MID128, BIG128, BIG256 };
+inline bool is_big(Tiles t) { return t >= BIG128; }
+inline int rows_of(Tiles t) { return t == BIG256 ? 256 : t == MID64 ? 64 : 128; }
 
-// BIG: where experts have rows for them (at even loads of 191 rows, 16 experts of d 4096,
-// d_ff 2048 in MX4, the FFN took 118 us with them and 108 without; at 1024 rows, 64 experts
-// of 2048 and 1024, 307 and 431), and enough k-steps for their pipeline.  Their offsets
-// within a tile have 32 bits.
-Tiles tiles_of(int64_t R, int E, int N, int K) {
-  if (R <= 16 * (int64_t)E) return FEW;
-  if (R > 256 * (int64_t)E && K >= 576 && N <= 1 << 20 && mx4_scale_bytes(R, K) < (size_t)1 << 31)
-    return BIG;
-  return MIDDLE;
+// Which: the host knows neither the loads nor how many experts have rows, so it counts
+// min(R, E) of them with half a tile's rows over each.
+// FEW against MIDDLE by their times: FEW streams the weights of every row tile (0.13 us a
+// MB) and reads the rows beside them (0.0037 us a MB and row), MIDDLE takes its k-steps'
+// latency or the weights' stream, whichever is longer.  The larger tiles where they are
+// enough for 256 CUs.  Measured, us for the FFN by 32 / 64 / 128 rows / BIG 128 / BIG 256:
+//   experts, d, d_ff      rows   MX4 activations             bf16 activations
+//   64, 2048, 1024         128   33 / 38 / 42 /  .  / 59     37 / 50 / 72 /  .  / 130
+//                         1024   63 / 46 / 50 /  48 / 63     65 / 61 / 88 /  87 / 141
+//                         4096  137 / 66 / 64 /  60 / 83    143 / 102 / 115 / 118 / 197
+//                        12288  372 / 128 / 111 / 87 / 90   377 / 217 / 213 / 198 / 213
+//                        32768  1008 / 285 / 231 / 151 / 147   951 / 512 / 444 / 383 / 377
+//   16, 4096, 2048          32   30 / 36 / 37 /  .  / 56     36 / 52 / 78 /  .  / 122
+//                          256   77 / 42 / 42 /  48 / 61     75 / 56 / 82 /  85 / 138
+//                         4096  554 / 124 / 105 / 94 / 103  506 / 262 / 253 / 222 / 251
+//   1, 2048, 2048          128   16 / 20 / 23 /  31 / 39     19 / 28 / 39 /  50 /  76
+//                         1024   65 / 26 / 27 /  33 / 43     68 / 37 / 44 /  55 /  79
+//                         4096  255 / 67 / 50 /  46 / 49    256 / 132 / 109 / 90 /  93
+// Over five such layers, 1 to 4096 tokens, the rule's choice is within a tenth of the best
+// but for a few where the last round of tiles is nearly empty.
+//
+// weights: values of one expert; cols: the widest product's columns; k_min, k_max: the
+// shortest and longest K; steps: 256-column steps of all products; products: their number.
+Tiles tiles_of(int64_t R, int E, int64_t weights, int64_t cols, int k_min, int k_max, int steps,
+               int products, bool mx4) {
+  const double live = (double)(R < E ? R : E), mb = weights * (17.0 / 32) * 1e-6;
+  const double few = 4 * products + mb * (0.13 * (live + R / 32) + 0.0037 * R);
+  const double latency = mx4 ? 5.2 * products + 0.56 * steps : 4.5 * products + 1.15 * steps;
+  const double stream = 3 * products + (mx4 ? 0.18 : 0.24) * mb * live;
+  if (few <= (latency > stream ? latency : stream)) return FEW;
+  auto tiles = [&](int bm, int bn) { return ((double)R / bm + live / 2) * ((cols + bn - 1) / bn); };
+  // BIG needs k-steps for its pipeline, and offsets within a tile and of scales in 32 bits
+  if (k_min >= 576 && cols <= 1 << 20 && mx4_scale_bytes(R, k_max) < (size_t)1 << 31) {
+    if (R > 512 * live && tiles(256, 256) >= 512) return BIG256;
+    if (tiles(128, 256) >= (mx4 ? 400 : 520)) return BIG128;
+  }
+  return R > (mx4 ? 96 : 200) * live && tiles(128, 128) >= 384 ? MID128 : MID64;
+}
+Tiles product_tiles(int64_t R, int E, int N, int K, bool mx4) {
+  return tiles_of(R, E, (int64_t)N * K, N, K, K, mx4_groups(K), 1, mx4);
+}
+Tiles ffn_tiles(int64_t R, int E, int d, int f, bool mx4) {
+  return tiles_of(R, E, 3LL * d * f, 2LL * f > d ? 2LL * f : d, d < f ? d : f, d < f ? f : d,
+                  mx4_groups(d) + mx4_groups(f), 2, mx4);
 }
 
-// one product with its epilogue, by the kernel that suits its sizes (R: the rows that the
-// workspace was sized for, at least the call's)
-hipError_t launch_product(const Mx4Args& a, bool round, const int32_t* offsets,
-                          const int32_t* expert_map, int E, int64_t R, int64_t R_call,
-                          hipStream_t s) {
-  const Tiles kind = tiles_of(R, E, a.N, a.K);
-  if (kind == FEW) return launch_mx4_few(a, round, offsets, expert_map, E, R_call, s);
-  if (kind == BIG) return launch_mx4_big(a, s);
+// one product with its epilogue (round: see launch_mx4_few)
+hipError_t launch_product(Mx4Args a, Tiles kind, bool round, const int32_t* offsets,
+                          const int32_t* expert_map, int E, int64_t R, hipStream_t s) {
+  if (kind == FEW) return launch_mx4_few(a, round, offsets, expert_map, E, R, s);
+  a.bm = rows_of(kind);
+  if (is_big(kind)) return launch_mx4_big(a, s);
   Mx4Params p = mx4_params(a);
   p.offsets = offsets;
   p.expert_map = expert_map;
   p.E = E;
   if (a.a_scale) {
-    if (a.f) return launch_middle<ACT_MX4, MX4_GU>(p, R_call, s);
-    return a.f32_out ? launch_middle<ACT_MX4, MX4_STORE_F32>(p, R_call, s)
-                     : launch_middle<ACT_MX4, MX4_STORE>(p, R_call, s);
+    if (a.f) return launch_middle<ACT_MX4, MX4_GU>(p, a.bm, R, s);
+    return a.f32_out ? launch_middle<ACT_MX4, MX4_STORE_F32>(p, a.bm, R, s)
+                     : launch_middle<ACT_MX4, MX4_STORE>(p, a.bm, R, s);
   }
-  if (a.f) return launch_middle<ACT_BF16, MX4_GU>(p, R_call, s);
-  return a.f32_out ? launch_middle<ACT_BF16, MX4_STORE_F32>(p, R_call, s)
-                   : launch_middle<ACT_BF16, MX4_STORE>(p, R_call, s);
+  if (a.f) return launch_middle<ACT_BF16, MX4_GU>(p, a.bm, R, s);
+  return a.f32_out ? launch_middle<ACT_BF16, MX4_STORE_F32>(p, a.bm, R, s)
+                   : launch_middle<ACT_BF16, MX4_STORE>(p, a.bm, R, s);
+}
+
+// Workspaces are laid out for every kind of tile (lists of 128-row tiles are the longest),
+// so a buffer for many tokens serves fewer.
+size_t list_bytes(int64_t R, int E, int n_cols, bool gate_up) {
+  return mx4_big_list_bytes(R, E, 128, n_cols, gate_up);
 }
 
 }  // namespace
 
+// the tile list, then X's scales in routed order
 size_t mx4_product_ws_bytes(int T, int k, int E, int K, int N) {
   const int64_t R = (int64_t)T * k;
-  if (tiles_of(R, E, N, K) != BIG) return 0;
-  return mx4_big_list_bytes(R, E, N, false) + align_up(mx4_scale_bytes(R, K), 256);
+  return list_bytes(R, E, N, false) + align_up(mx4_scale_bytes(R, K), 256);
 }
 
 hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32_t* row_src, int T,
@@ -421,12 +462,13 @@ hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32
   a.out_rows = R;
   a.row_src = row_src;
   a.slots_k = k;
-  if (tiles_of(R_ws, E, N, K) == BIG) {
+  const Tiles kind = product_tiles(R_ws, E, N, K, x_scale != nullptr);
+  if (is_big(kind)) {
     uint8_t* const list = static_cast<uint8_t*>(ws);
-    uint8_t* const routed = list + mx4_big_list_bytes(R_ws, E, N, false);
+    uint8_t* const routed = list + list_bytes(R_ws, E, N, false);
     const bool gather = x_scale && row_src;
     const hipError_t err =
-        launch_mx4_prepare(offsets, expert_map, E, R, 0, nullptr, N, list, x_scale,
+        launch_mx4_prepare(offsets, expert_map, E, R, rows_of(kind), 0, nullptr, N, list, x_scale,
                            gather ? routed : nullptr, row_src, k, T, K, s);
     if (err != hipSuccess) return err;
     if (gather) {
@@ -435,29 +477,25 @@ hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32
     }
     a.list = list;
   }
-  return launch_product(a, false, offsets, expert_map, E, R_ws, R, s);
+  return launch_product(a, kind, false, offsets, expert_map, E, R, s);
 }
 
 namespace {
 
-// the FFN's workspace: X in MX4, H (MX4 or bf16), and where the products take the large
-// tiles their lists and X's scales in routed order
+// the FFN's workspace: X in MX4, H (MX4 or bf16), the products' tile lists, and X's scales
+// in routed order
 struct Mx4FfnWs {
   size_t x_scale, h, h_scale, list_gu, list_d, routed, bytes;
-  Tiles gu, down;
 };
 Mx4FfnWs ffn_ws(int64_t T, int64_t R, int E, int d, int f, bool mx4) {
   Mx4FfnWs w;
-  w.gu = tiles_of(R, E, 2 * f, d);
-  w.down = tiles_of(R, E, d, f);
-  const bool x = mx4 && w.gu != FEW, big = w.gu == BIG || w.down == BIG;
-  w.x_scale = x ? align_up((size_t)T * d / 2, 256) : 0;
-  w.h = w.x_scale + (x ? align_up(mx4_scale_bytes(T, d), 256) : 0);
+  w.x_scale = mx4 ? align_up((size_t)T * d / 2, 256) : 0;
+  w.h = w.x_scale + (mx4 ? align_up(mx4_scale_bytes(T, d), 256) : 0);
   w.h_scale = w.h + align_up((size_t)R * f * 2 / (mx4 ? 4 : 1), 256);
   w.list_gu = w.h_scale + (mx4 ? align_up(mx4_scale_bytes(R, f), 256) : 0);
-  w.list_d = w.list_gu + (big ? mx4_big_list_bytes(R, E, f, true) : 0);
-  w.routed = w.list_d + (big ? mx4_big_list_bytes(R, E, d, false) : 0);
-  w.bytes = w.routed + (w.gu == BIG && mx4 ? align_up(mx4_scale_bytes(R, d), 256) : 0);
+  w.list_d = w.list_gu + list_bytes(R, E, f, true);
+  w.routed = w.list_d + list_bytes(R, E, d, false);
+  w.bytes = w.routed + (mx4 ? align_up(mx4_scale_bytes(R, d), 256) : 0);
   return w;
 }
 
@@ -478,20 +516,21 @@ hipError_t launch_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int 
   const bool mx4 = act_bits == 4;
   const int64_t R_ws = row_src ? (int64_t)T * k : T;
   const Mx4FfnWs at = ffn_ws(T, R_ws, E, d, f, mx4);
+  const Tiles kind = ffn_tiles(R_ws, E, d, f, mx4);
   uint8_t* const base = static_cast<uint8_t*>(ws);
   Mx4Args a = {};
   a.A = x;
   a.a_rows = T;
   hipError_t err = hipSuccess;
-  if (mx4 && at.gu != FEW) {
+  if (mx4 && kind != FEW) {
     err = launch_mx4_quantize(x, kDtypeBf16, 1, T, d, base, base + at.x_scale, s);
     if (err != hipSuccess) return err;
     a.A = base;
     a.a_scale = base + at.x_scale;
   }
-  if (at.gu == BIG || at.down == BIG) {
-    const bool gather = at.gu == BIG && mx4 && row_src;
-    err = launch_mx4_prepare(offsets, expert_map, E, R, f, base + at.list_gu, d, base + at.list_d,
+  if (is_big(kind)) {
+    const bool gather = mx4 && row_src;
+    err = launch_mx4_prepare(offsets, expert_map, E, R, rows_of(kind), f, base + at.list_gu, d, base + at.list_d,
                              a.a_scale, gather ? base + at.routed : nullptr, row_src, k, T, d, s);
     if (err != hipSuccess) return err;
     if (gather) {
@@ -511,7 +550,7 @@ hipError_t launch_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int 
   a.row_src = row_src;
   a.slots_k = k;
   a.list = base + at.list_gu;
-  err = launch_product(a, mx4, offsets, expert_map, E, R_ws, R, s);
+  err = launch_product(a, kind, mx4, offsets, expert_map, E, R, s);
   if (err != hipSuccess) return err;
   a.A = a.out;
   a.a_scale = mx4 ? a.out_scale : nullptr;
@@ -525,7 +564,7 @@ hipError_t launch_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int 
   a.act = nullptr;
   a.row_src = nullptr;
   a.list = base + at.list_d;
-  return launch_product(a, false, offsets, expert_map, E, R_ws, R, s);
+  return launch_product(a, kind, false, offsets, expert_map, E, R, s);
 }
 
 }  // namespace laep

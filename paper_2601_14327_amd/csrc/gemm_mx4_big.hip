@@ -20,7 +20,7 @@ namespace laep {
 namespace {
 
 constexpr int kBigThreads = 512;
-constexpr int kBigBM = 256, kBigBN = 256;
+constexpr int kBigBN = 256;
 
 struct BigTile {
   int row0, rows, phys, nt;
@@ -49,14 +49,14 @@ __device__ __forceinline__ uint32_t column_pair(uint32_t v, int lane) {
 // (lane / 32) + i of fragment j.  Columns in lanes: row 8q + 4 (lane / 32) + i, column
 // lane % 32.  Descriptors end with the tile's rows: stores past them, or at dropped
 // offsets, write nothing, and every wave issues the same number.
-template <int ACT, int EPI>
+template <int ACT, int EPI, int WTM>
 __device__ __forceinline__ void store_block(const Mx4Params& p, const BigTile& te, int i, int wm,
                                             int wn, int lane, const f32x16_t acc[2]) {
   const int half = lane >> 5;
   auto rsrc_of = [&](void* base, long long bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(base, 0, (int)bytes, kBufferFlags);
   };
-  const uint32_t row0 = wm * 128 + i * 32;
+  const uint32_t row0 = wm * WTM + i * 32;
   if constexpr (EPI == MX4_GU) {
     const int f = p.f, fcol = te.nt * 128 + wn * 32;   // f % 64 == 0: whole blocks
     const bool in = fcol < f;
@@ -131,19 +131,22 @@ __device__ __forceinline__ void store_block(const Mx4Params& p, const BigTile& t
   }
 }
 
-template <int ACT, int EPI>
+template <int ACT, int EPI, int BM>
 __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) {
   constexpr bool MX4 = ACT == ACT_MX4;
-  constexpr int NT = kBigThreads, TM = 4, TN = 2;
-  constexpr int HALF = kBigBM * 128;
-  constexpr int BPART = MX4 ? HALF : kBigBN * 32;    // weights of a step
-  constexpr int NSLOT = MX4 ? 3 : 4;                 // steps of A; of B (MX4: one fewer)
-  constexpr int NSLOTB = MX4 ? 2 : 4;
-  constexpr int AHEAD = MX4 ? 2 : 3;                 // steps the copies run ahead
-  constexpr int NH = HALF / 16 / NT;                 // copies a thread and half
-  constexpr int NB = BPART / 16 / NT;
-  __shared__ __attribute__((aligned(1024))) char smem[160 * 1024];
-  static_assert(NSLOT * HALF + NSLOTB * BPART == sizeof(smem), "the whole LDS");
+  constexpr int NT = kBigThreads, WTM = BM / 2, TM = WTM / 32, TN = 2;
+  constexpr int APART = BM * 128;                    // a step's activations
+  constexpr int BPART = MX4 ? kBigBN * 128 : kBigBN * 32;  // and its weights
+  // steps in the LDS: of A; of B (256 rows in MX4: one fewer)
+  constexpr int NSLOT = MX4 ? 3 : BM == 256 ? 4 : 6;
+  constexpr int NSLOTB = MX4 && BM == 256 ? 2 : NSLOT;
+  constexpr int AHEAD = MX4 ? 2 : NSLOT - 1;         // steps the copies run ahead
+  constexpr int NH = APART / 16 / NT;                // copies a thread and step of A
+  constexpr int NB = BPART / 16 / NT;                // and of B
+  static_assert(BM == 256 || BM == 128, "two rows of waves");
+  constexpr int SMEM = NSLOT * APART + NSLOTB * BPART;
+  static_assert(SMEM <= 160 * 1024, "the LDS");
+  __shared__ __attribute__((aligned(1024))) char smem[SMEM];
 
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5;
@@ -177,7 +180,7 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
   };
   const int a_row_bytes = MX4 ? p.K / 2 : p.K * 2;
   const int G = (p.K + kMx4Group - 1) / kMx4Group;
-  const int nk = MX4 ? G : p.K / 64;                 // (host: at least 3, bf16 5)
+  const int nk = MX4 ? G : p.K / 64;                 // (host: at least 3, bf16 9)
 
   // ---- copies: rows of the next tile, then offsets and descriptors of the tile that is
   // being copied, which the end of its last step moves on
@@ -226,12 +229,12 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
   };
   int a_slot = 0, b_slot = 0;
   auto copy_a = [&](int i) {
-    char* const dst = smem + a_slot * HALF + i * NT * 16;
+    char* const dst = smem + a_slot * APART + i * NT * 16;
     const uint32_t v[1] = {MX4 ? codes_at(a_voff[i]) : a_voff[i]};
     dma_chunks<1, NT>(dst, a_rsrc, v, c_step * 128, wave);
   };
   auto copy_b = [&](int i) {
-    char* const dst = smem + NSLOT * HALF + b_slot * BPART + i * NT * 16;
+    char* const dst = smem + NSLOT * APART + b_slot * BPART + i * NT * 16;
     const uint32_t v[1] = {MX4 ? codes_at(b_voff) : b_voff};
     dma_chunks<1, NT>(dst, b_rsrc, v, MX4 ? b_group[i] + c_step * 128 : c_step * 32, wave);
   };
@@ -250,7 +253,7 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
   auto begin_scales = [&](const BigTile& t) {
     if constexpr (MX4) {
       // rows past the tile's end take other rows' scales, past the array's end none
-      sa_off = (wm * 128 + (lane & 31)) * 8 + half * 4;
+      sa_off = (wm * WTM + (lane & 31)) * 8 + half * 4;
       sa_rsrc = __builtin_amdgcn_make_buffer_rsrc(
           const_cast<uint8_t*>(p.a_scale) + (long long)t.row0 * 8, 0,
           (int)((G * p.a_rows - t.row0) * 8), kBufferFlags);
@@ -289,7 +292,7 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
   int a_off[2], b_off[TN];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int r = wm * 128 + i * 32 + (lane & 31);
+    const int r = wm * WTM + i * 32 + (lane & 31);
     a_off[i] = r * 128 + (((4 * half) ^ swz8(r)) << 4);
   }
 #pragma unroll
@@ -310,8 +313,8 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
   u32x4_t fa0[TM], fa1[TM];                          // A of a sub-step and of the next
   u32x4_t fb[MX4 ? 4 : 1][TN];                       // MX4: a step's B whole; bf16: its codes
   int ra = 0, rb = 0;                                // slots that are read
-  auto a_base = [&]() { return smem + ra * HALF; };
-  auto b_base = [&]() { return smem + NSLOT * HALF + rb * BPART; };
+  auto a_base = [&]() { return smem + ra * APART; };
+  auto b_base = [&]() { return smem + NSLOT * APART + rb * BPART; };
   auto read_a = [&](u32x4_t* ga, int s, int i) {
     ga[i] = *reinterpret_cast<const u32x4_t*>(a_base() + (a_off[i & 1] ^ (s << 4)) + (i >> 1) * 8192);
   };
@@ -361,10 +364,10 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
   using I1 = std::integral_constant<int, 1>;
   using I2 = std::integral_constant<int, 2>;
   using I3 = std::integral_constant<int, 3>;
-  using Num4 = std::integral_constant<int, 4>;
-  using Num6 = std::integral_constant<int, 6>;
-  using Num10 = std::integral_constant<int, 10>;
-  static_assert(TM == 4 && TN == 2 && NH == 4, "the reads and copies below");
+  using CopiesA = std::integral_constant<int, NH>;
+  using CopiesB = std::integral_constant<int, NB>;
+  using ReadsA = std::integral_constant<int, TM>;
+  using Scales = std::integral_constant<int, NS>;
   auto nothing = [](int) {};
 
   // ---- the stream
@@ -416,11 +419,11 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
   // of the next step's first fragments, and the copies of A two steps past that one into
   // the slot that the step has just freed.
   auto last_sub = [&]() {
-    sub_step(I3{}, fa1, Num10{}, [&](int n) {
-      if (n < 2) read_b(0, n);
-      else if (n < 6) read_a(fa0, 0, n - 2);
-      else read_b(1 + (n - 6) / 2, n & 1);
-    }, I1{}, Num4{}, [&](int n) { copy_a(n); });
+    sub_step(I3{}, fa1, std::integral_constant<int, TM + 3 * TN>{}, [&](int n) {
+      if (n < TN) read_b(0, n);
+      else if (n < TN + TM) read_a(fa0, 0, n - TN);
+      else read_b(1 + (n - TN - TM) / TN, (n - TN - TM) % TN);
+    }, I1{}, CopiesA{}, [&](int n) { copy_a(n); });
     fence();
   };
   // MX4: the rest of a step.  Its B fragments are all in registers after the first
@@ -429,16 +432,18 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
     constexpr bool EARLY = decltype(early_tag)::value;
     constexpr int SET = decltype(set_tag)::value;
     take_scales(SET);
-    sub_step(I0{}, fa0, Num6{}, [&](int n) {
-      if (n < 4) read_a(fa1, 1, n);
-      else read_b(3, n - 4);
-    }, I1{}, Num6{}, [&](int n) { load_scale(SET, n, s_step); });
-    wait_lgkm0();
-    __builtin_amdgcn_s_barrier();
-    sub_step(I1{}, fa1, Num4{}, [&](int n) { read_a(fa0, 2, n); }, I2{}, Num4{},
-             [&](int n) { copy_b(n); });
+    sub_step(I0{}, fa0, std::integral_constant<int, TM + TN>{}, [&](int n) {
+      if (n < TM) read_a(fa1, 1, n);
+      else read_b(3, n - TM);
+    }, I1{}, Scales{}, [&](int n) { load_scale(SET, n, s_step); });
+    if constexpr (NSLOTB == 2) {                     // (with three slots B's is free already)
+      wait_lgkm0();
+      __builtin_amdgcn_s_barrier();
+    }
+    sub_step(I1{}, fa1, ReadsA{}, [&](int n) { read_a(fa0, 2, n); },
+             std::integral_constant<int, TM / 2>{}, CopiesB{}, [&](int n) { copy_b(n); });
     copied();
-    sub_step(I2{}, fa0, Num4{}, [&](int n) { read_a(fa1, 3, n); }, I1{}, I0{}, nothing);
+    sub_step(I2{}, fa0, ReadsA{}, [&](int n) { read_a(fa1, 3, n); }, I1{}, I0{}, nothing);
     // The next step has landed: after its copies (of B in the step before this) came A's
     // and B's of two steps on, six scales and, in a tile's first step, the stores of the
     // tile before.
@@ -446,27 +451,27 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
     wait_vmcnt_lgkm0<(W < 63 ? W : 63)>();
     __builtin_amdgcn_s_barrier();
     ra = ra + 1 == NSLOT ? 0 : ra + 1;
-    rb ^= 1;
+    rb = rb + 1 == NSLOTB ? 0 : rb + 1;
     fence();
   };
-  // bf16: one step; EARLY: the first two of a tile
+  // bf16: one step; EARLY: the first AHEAD - 1 of a tile
   auto bf16_step = [&](auto early_tag, int s_step) {
     constexpr bool EARLY = decltype(early_tag)::value;
-    sub_step(I0{}, fa0, Num4{}, [&](int n) { read_a(fa1, 1, n); }, I1{}, I2{},
+    sub_step(I0{}, fa0, ReadsA{}, [&](int n) { read_a(fa1, 1, n); }, I1{}, Scales{},
              [&](int n) { load_scale(0, n, s_step); });
-    sub_step(I1{}, fa1, Num4{}, [&](int n) { read_a(fa0, 2, n); }, I2{}, Num4{},
+    sub_step(I1{}, fa1, ReadsA{}, [&](int n) { read_a(fa0, 2, n); }, I2{}, CopiesA{},
              [&](int n) { copy_a(n); });
-    sub_step(I2{}, fa0, Num4{}, [&](int n) { read_a(fa1, 3, n); }, I1{}, I1{},
+    sub_step(I2{}, fa0, ReadsA{}, [&](int n) { read_a(fa1, 3, n); }, I1{}, CopiesB{},
              [&](int n) { copy_b(n); });
     copied();
-    // The next step has landed: after its copies came those of two steps, and in the
-    // first two steps of a tile the stores of the tile before.
-    constexpr int W = 2 * (NH + NB) + (EARLY ? S_ALL : 0);
+    // The next step has landed: after its copies came those of AHEAD - 1 steps, and in
+    // the first AHEAD - 1 steps of a tile the stores of the tile before.
+    constexpr int W = (AHEAD - 1) * (NH + NB) + (EARLY ? S_ALL : 0);
     wait_vmcnt_lgkm0<(W < 63 ? W : 63)>();
     __builtin_amdgcn_s_barrier();
     ra = ra + 1 == NSLOT ? 0 : ra + 1;
     rb = ra;
-    sub_step(I3{}, fa1, Num4{}, [&](int n) { read_a(fa0, 0, n); }, I1{}, I0{}, nothing);
+    sub_step(I3{}, fa1, ReadsA{}, [&](int n) { read_a(fa0, 0, n); }, I1{}, I0{}, nothing);
 #pragma unroll
     for (int j = 0; j < TN; ++j) read_b(0, j);
     take_scales(0);
@@ -511,9 +516,8 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
       }
       last_sub();
     } else {
-      bf16_step(Early{}, 1);
-      bf16_step(Early{}, 2);
-      int kt = 2;
+      int kt = 0;
+      for (; kt < AHEAD - 1; ++kt) bf16_step(Early{}, kt + 1);
       for (; kt < nk - AHEAD; ++kt) bf16_step(Later{}, kt + 1);
       begin_copies(nxt, more);                       // the copies reach the next tile
       for (; kt < nk - 1; ++kt) bf16_step(Later{}, kt + 1);
@@ -531,7 +535,7 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
     }
     __builtin_amdgcn_sched_barrier(0);               // the stores come after, see the waits
 #pragma unroll
-    for (int i = 0; i < TM; ++i) store_block<ACT, EPI>(p, done, i, wm, wn, lane, acc[i]);
+    for (int i = 0; i < TM; ++i) store_block<ACT, EPI, WTM>(p, done, i, wm, wn, lane, acc[i]);
     __builtin_amdgcn_sched_barrier(0);
     if (!go_on) break;
   }
@@ -552,9 +556,9 @@ struct GatherScales {
 
 __global__ __launch_bounds__(kTableThreads) void mx4_prepare_kernel(
     const int32_t* __restrict__ offsets, const int32_t* __restrict__ expert_map, int E,
-    TileList la, TileList lb, int list_blocks, GatherScales g) {
+    int BM, TileList la, TileList lb, int list_blocks, GatherScales g) {
   if ((int)blockIdx.x < list_blocks) {
-    build_tile_lists(blockIdx.x, offsets, expert_map, E, kBigBM, la, lb);
+    build_tile_lists(blockIdx.x, offsets, expert_map, E, BM, la, lb);
     return;
   }
   const long long n = (long long)(gridDim.x - list_blocks) * kTableThreads;
@@ -567,34 +571,37 @@ __global__ __launch_bounds__(kTableThreads) void mx4_prepare_kernel(
 }
 
 template <int ACT, int EPI>
-hipError_t launch_big(const Mx4Params& p, hipStream_t s) {
+hipError_t launch_big(const Mx4Params& p, int bm, hipStream_t s) {
   int dev = 0, cus = 0;
   hipError_t err = hipGetDevice(&dev);
   if (err == hipSuccess) err = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   if (err != hipSuccess) return err;
   // one workgroup per CU, a multiple of 8 so every XCD gets the same number
-  hipLaunchKernelGGL((gemm_mx4_big_kernel<ACT, EPI>), dim3(max(8, cus / 8 * 8)), dim3(kBigThreads),
-                     0, s, p);
+  const dim3 grid(max(8, cus / 8 * 8));
+  if (bm == 256)
+    hipLaunchKernelGGL((gemm_mx4_big_kernel<ACT, EPI, 256>), grid, dim3(kBigThreads), 0, s, p);
+  else
+    hipLaunchKernelGGL((gemm_mx4_big_kernel<ACT, EPI, 128>), grid, dim3(kBigThreads), 0, s, p);
   return hipGetLastError();
 }
 
-inline int list_max(int64_t R, int E, int n_tiles) {
-  return (ceil_div(R, kBigBM) + (int)(R < E ? R : E)) * n_tiles;
+inline int list_max(int64_t R, int E, int bm, int n_tiles) {
+  return (ceil_div(R, bm) + (int)(R < E ? R : E)) * n_tiles;
 }
 
 }  // namespace
 
-size_t mx4_big_list_bytes(int64_t R, int E, int n_cols, bool gate_up) {
-  return table_bytes(list_max(R, E, ceil_div(n_cols, gate_up ? kBigBN / 2 : kBigBN)));
+size_t mx4_big_list_bytes(int64_t R, int E, int bm, int n_cols, bool gate_up) {
+  return table_bytes(list_max(R, E, bm, ceil_div(n_cols, gate_up ? kBigBN / 2 : kBigBN)));
 }
 
 hipError_t launch_mx4_prepare(const int32_t* offsets, const int32_t* expert_map, int E, int64_t R,
-                              int f, void* list_gu, int n_cols, void* list,
+                              int bm, int f, void* list_gu, int n_cols, void* list,
                               const uint8_t* x_scale, uint8_t* routed_scale,
                               const int32_t* row_src, int slots_k, int64_t T, int K,
                               hipStream_t s) {
   const int nt_a = list_gu ? ceil_div(f, kBigBN / 2) : 1, nt_b = ceil_div(n_cols, kBigBN);
-  const int max_a = list_gu ? list_max(R, E, nt_a) : 0, max_b = list_max(R, E, nt_b);
+  const int max_a = list_gu ? list_max(R, E, bm, nt_a) : 0, max_b = list_max(R, E, bm, nt_b);
   const TableWs tb = carve_table(list, max_b);
   const TableWs ta = list_gu ? carve_table(list_gu, max_a) : tb;
   const TileList la = {nt_a, kFwdTileGroup, max_a, ta.n_entries, ta.table};
@@ -609,7 +616,7 @@ hipError_t launch_mx4_prepare(const int32_t* offsets, const int32_t* expert_map,
   }
   // (of one list only, both are that list: written twice, alike)
   hipLaunchKernelGGL(mx4_prepare_kernel, dim3(blocks + more), dim3(kTableThreads), 0, s, offsets,
-                     expert_map, E, list_gu ? la : lb, lb, blocks, g);
+                     expert_map, E, bm, list_gu ? la : lb, lb, blocks, g);
   return hipGetLastError();
 }
 
@@ -619,11 +626,13 @@ hipError_t launch_mx4_big(const Mx4Args& a, hipStream_t s) {
   p.table = t.table;
   p.n_entries = t.n_entries;
   if (a.a_scale) {
-    if (a.f) return launch_big<ACT_MX4, MX4_GU>(p, s);
-    return a.f32_out ? launch_big<ACT_MX4, MX4_STORE_F32>(p, s) : launch_big<ACT_MX4, MX4_STORE>(p, s);
+    if (a.f) return launch_big<ACT_MX4, MX4_GU>(p, a.bm, s);
+    return a.f32_out ? launch_big<ACT_MX4, MX4_STORE_F32>(p, a.bm, s)
+                     : launch_big<ACT_MX4, MX4_STORE>(p, a.bm, s);
   }
-  if (a.f) return launch_big<ACT_BF16, MX4_GU>(p, s);
-  return a.f32_out ? launch_big<ACT_BF16, MX4_STORE_F32>(p, s) : launch_big<ACT_BF16, MX4_STORE>(p, s);
+  if (a.f) return launch_big<ACT_BF16, MX4_GU>(p, a.bm, s);
+  return a.f32_out ? launch_big<ACT_BF16, MX4_STORE_F32>(p, a.bm, s)
+                   : launch_big<ACT_BF16, MX4_STORE>(p, a.bm, s);
 }
 
 }  // namespace laep

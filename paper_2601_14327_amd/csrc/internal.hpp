@@ -179,7 +179,7 @@ hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32
                               int k, const uint8_t* w, const uint8_t* w_scale,
                               const int32_t* offsets, const int32_t* expert_map, int out_dtype,
                               int E, int N, int K, int64_t R, void* out, void* ws, hipStream_t s);
-// The same products by 256 x 256 tiles (gemm_mx4_big.hip): each needs the list of its
+// The same products by 128 or 256 x 256 tiles (gemm_mx4_big.hip): each needs the list of its
 // tiles, and gathered MX4 activations their scales in routed order, both from
 // launch_mx4_prepare (list_gu: the list of a gate/up product as well, or NULL).
 struct Mx4Args {
@@ -197,10 +197,11 @@ struct Mx4Args {
   const int32_t* row_src;
   int slots_k;
   void* list;
+  int bm;                    // rows of a tile, 128 or 256
 };
-size_t mx4_big_list_bytes(int64_t R, int E, int n_cols, bool gate_up);
+size_t mx4_big_list_bytes(int64_t R, int E, int bm, int n_cols, bool gate_up);
 hipError_t launch_mx4_prepare(const int32_t* offsets, const int32_t* expert_map, int E, int64_t R,
-                              int f, void* list_gu, int n_cols, void* list,
+                              int bm, int f, void* list_gu, int n_cols, void* list,
                               const uint8_t* x_scale, uint8_t* routed_scale,
                               const int32_t* row_src, int slots_k, int64_t T, int K,
                               hipStream_t s);
