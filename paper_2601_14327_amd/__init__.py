@@ -42,6 +42,7 @@ and experts in microscaled 4 bits (MX4; Mx4 holds a matrix's codes and scales):
     laep_calib_copy, laep_calib_read,  measurement calls (attained peaks,
     laep_calib_mfma                    the router's feed bound)
     laep_ffn_fwd_row_tile              which kernels a forward call runs
+    laep_mx4_product_tile, laep_mx4_ffn_tile  (and the calls at MX4 weights)
 """
 from ._lib import (  # noqa: F401
     LAEP_ACT8_BLOCK, LAEP_BF16, LAEP_CALL_BALANCE, LAEP_CALL_FFN_BWD, LAEP_CALL_FFN_FWD,
@@ -57,6 +58,8 @@ from .api import (  # noqa: F401
     laep_compact_experts,
     laep_expert_pruning,
     laep_ffn_fwd_row_tile,
+    laep_mx4_ffn_tile,
+    laep_mx4_product_tile,
     laep_prune_mask,
     laep_rearrange,
     laep_repack_experts,

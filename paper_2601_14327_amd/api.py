@@ -1009,3 +1009,20 @@ def laep_calib_mfma(n_workgroups: int, iters: int, out: torch.Tensor):
 def laep_ffn_fwd_row_tile(R: int, E: int, d_model: int, d_ff: int) -> int:
     """Rows per tile (32, 64, 128 or 256) of the bf16 forward FFN at these sizes."""
     return int(lib().laep_ffn_fwd_row_tile(int(R), int(E), int(d_model), int(d_ff)))
+
+
+def laep_mx4_product_tile(R: int, E: int, N: int, K: int, act_bits: int = 16) -> tuple:
+    """(rows, columns) of the tiles of moe_mx4_grouped_product for R = T k rows (T without
+    row_src); (0, 0) for sizes that it refuses."""
+    cols = ctypes.c_int(0)
+    rows = lib().laep_mx4_product_tile(int(R), int(E), int(N), int(K), int(act_bits),
+                                       ctypes.byref(cols))
+    return int(rows), cols.value
+
+
+def laep_mx4_ffn_tile(R: int, E: int, d_model: int, d_ff: int, act_bits: int = 16) -> tuple:
+    """(rows, columns) of the tiles of moe_grouped_ffn_fwd_mx4, likewise."""
+    cols = ctypes.c_int(0)
+    rows = lib().laep_mx4_ffn_tile(int(R), int(E), int(d_model), int(d_ff), int(act_bits),
+                                   ctypes.byref(cols))
+    return int(rows), cols.value

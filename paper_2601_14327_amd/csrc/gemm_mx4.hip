@@ -361,7 +361,8 @@ hipError_t launch_middle(Mx4Params p, int bm, int64_t R, hipStream_t s) {
 // 128, or the persistent 128 or 256 x 256 (BIG).
 enum Tiles { FEW, MID64, MID128, BIG128, BIG256 };
 inline bool is_big(Tiles t) { return t >= BIG128; }
-inline int rows_of(Tiles t) { return t == BIG256 ? 256 : t == MID64 ? 64 : 128; }
+inline int rows_of(Tiles t) { return t == BIG256 ? 256 : t == FEW ? 32 : t == MID64 ? 64 : 128; }
+inline int cols_of(Tiles t) { return is_big(t) ? 256 : t == FEW ? 64 : 128; }
 
 // Which: the host knows neither the loads nor how many experts have rows, so it counts
 // min(R, E) of them with half a tile's rows over each.
@@ -436,6 +437,18 @@ size_t list_bytes(int64_t R, int E, int n_cols, bool gate_up) {
 }
 
 }  // namespace
+
+int mx4_product_tile(int64_t R, int E, int N, int K, bool mx4, int* cols) {
+  const Tiles t = product_tiles(R, E, N, K, mx4);
+  if (cols) *cols = cols_of(t);
+  return rows_of(t);
+}
+
+int mx4_ffn_tile(int64_t R, int E, int d, int f, bool mx4, int* cols) {
+  const Tiles t = ffn_tiles(R, E, d, f, mx4);
+  if (cols) *cols = cols_of(t);
+  return rows_of(t);
+}
 
 // the tile list, then X's scales in routed order
 size_t mx4_product_ws_bytes(int T, int k, int E, int K, int N) {

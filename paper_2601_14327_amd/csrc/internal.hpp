@@ -174,6 +174,9 @@ hipError_t launch_mx4_quantize(const void* src, int dtype, int n, int64_t R, int
 hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scale, int dtype, int n,
                                  int64_t R, int C, void* out, hipStream_t s);
 // Products at MX4 weights; x_scale NULL: x is bf16; row_src NULL: rows in order.
+// The tiles of the products and of the FFN: rows, and in cols (if not NULL) the columns.
+int mx4_product_tile(int64_t R, int E, int N, int K, bool mx4, int* cols);
+int mx4_ffn_tile(int64_t R, int E, int d, int f, bool mx4, int* cols);
 size_t mx4_product_ws_bytes(int T, int k, int E, int K, int N);
 hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32_t* row_src, int T,
                               int k, const uint8_t* w, const uint8_t* w_scale,

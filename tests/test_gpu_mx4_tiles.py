@@ -1,0 +1,115 @@
+"""The products at MX4 weights in every tile that their rule takes, against the float64
+oracle: odd and even numbers of k-steps, ragged experts, column tiles past the matrix, more
+tiles than workgroups.  Bounds as in test_gpu_mx4.py."""
+import functools
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_14327_amd as laep
+from _gpu import case, dev, host
+from oracle import mx4
+from oracle.numerics import round_bf16
+from test_gpu_mx4 import DT, _bound, _ffn_check, _ffn_inputs, _i32, _mx4, _routing
+
+pytestmark = pytest.mark.gpu
+
+PRODUCTS = [   # rows and columns of the tiles; T, k, E, dead, N, K
+    ((32, 64), 90, 1, 4, 1, 128, 576), ((64, 128), 1500, 2, 16, 3, 1088, 704),
+    ((128, 128), 6300, 1, 2, 0, 1024, 320), ((128, 128), 2100, 3, 3, 1, 1088, 192),
+    # 3, 3, 4, 5, 5 steps of 256 columns; 9 and more of 64
+    ((128, 256), 8100, 1, 20, 0, 2048, 576), ((128, 256), 1100, 8, 20, 3, 1984, 640),
+    ((128, 256), 4100, 2, 19, 0, 2112, 1024), ((128, 256), 8500, 1, 20, 5, 2048, 1216),
+    ((128, 256), 33000, 1, 80, 9, 448, 1088),
+    ((256, 256), 4300, 2, 2, 0, 3904, 576), ((256, 256), 16500, 2, 3, 0, 1088, 640),
+    ((256, 256), 17000, 1, 6, 1, 1856, 1024), ((256, 256), 35000, 1, 1, 0, 832, 1216),
+    ((256, 256), 70000, 1, 5, 2, 448, 832)]
+
+
+@functools.lru_cache(1)     # (shared by the types of one size)
+def _operands(T, k, E, dead, N, K):
+    g = np.random.default_rng(T + N + K)
+    routing = _routing(g, T, k, E, dead, skew=1.0)
+    x = round_bf16(g.normal(size=(T, K)))
+    return (*routing, x, mx4.quantize(g.normal(size=(E - dead, N, K)) * 0.05), mx4.quantize(x))
+
+
+@functools.lru_cache(1)
+def _reference(T, k, E, dead, N, K, act):
+    row_src, offsets, emap, x, qw, qx = _operands(T, k, E, dead, N, K)
+    xv = mx4.dequantize(*qx) if act == 4 else x
+    return mx4.grouped_product(xv[row_src // k], mx4.dequantize(*qw), offsets, emap)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", [4, 16])
+@pytest.mark.parametrize("tile,T,k,E,dead,N,K", PRODUCTS)
+def test_product(tile, T, k, E, dead, N, K, act, dtype):
+    case(f"mx4 product tile={tile} T={T} k={k} E={E} dead={dead} N={N} K={K} act={act} {dtype}")
+    assert laep.laep_mx4_product_tile(T * k, E, N, K, act) == tile
+    row_src, offsets, emap, x, qw, qx = _operands(T, k, E, dead, N, K)
+    ref, mag = _reference(T, k, E, dead, N, K, act)
+    live = ~np.isnan(ref)            # (the oracle's mark: rows of experts without a slot)
+    out = torch.full((T * k, N), 7.0, dtype=DT[dtype], device="cuda")
+    args = (_mx4(qx) if act == 4 else dev(x, torch.bfloat16), _mx4(qw), _i32(offsets))
+    kw = dict(row_src=_i32(row_src), k=k, expert_map=_i32(emap), dtype=DT[dtype])
+    laep.moe_mx4_grouped_product(*args, out=out, **kw)
+    got = host(out)
+    assert (np.abs(got - ref) <= _bound(mag, ref, K, dtype))[live].all()
+    assert (got[~live] == 7.0).all()
+    again = laep.moe_mx4_grouped_product(*args, out=torch.full_like(out, 7.0), **kw)
+    assert torch.equal(again, out)
+
+
+FFNS = [   # rows and columns of the tiles; T, k, E, dead, d, f
+    ((64, 128), 1500, 2, 16, 3, 320, 704), ((128, 128), 3200, 2, 2, 0, 320, 512),
+    ((128, 256), 1000, 8, 20, 0, 1088, 1024), ((128, 256), 8800, 1, 20, 2, 576, 1216),
+    ((256, 256), 16500, 2, 2, 0, 576, 576), ((256, 256), 9000, 1, 2, 0, 640, 1984)]
+
+
+@pytest.mark.parametrize("act", [4, 16])
+@pytest.mark.parametrize("tile,T,k,E,dead,d,f", FFNS)
+def test_ffn(tile, T, k, E, dead, d, f, act):
+    case(f"mx4 ffn tile={tile} T={T} k={k} E={E} dead={dead} d={d} f={f} act={act}")
+    assert laep.laep_mx4_ffn_tile(T * k, E, d, f, act) == tile
+    x, row_src, offsets, emap, gu, dn = _ffn_inputs(T + d + f, T, k, E, dead, d, f)
+    kw = dict(row_src=_i32(row_src), k=k, act_bits=act, expert_map=_i32(emap))
+    args = (dev(x, torch.bfloat16), _mx4(gu), _mx4(dn), _i32(offsets))
+    y, a = laep.moe_grouped_ffn_fwd_mx4(*args, save_act=act == 16, **kw)
+    _ffn_check(y, x, row_src, offsets, emap, gu, dn, k, act, a)
+    again, none = laep.moe_grouped_ffn_fwd_mx4(*args, **kw)
+    assert none is None and torch.equal(y, again)
+    own, _ = laep.moe_grouped_ffn_fwd_mx4(dev(x[row_src // k], torch.bfloat16), *args[1:],
+                                          act_bits=act, expert_map=_i32(emap))
+    assert torch.equal(y, own)
+
+
+@pytest.mark.parametrize("act", [4, 16])
+@pytest.mark.parametrize("tile,T,E,N,K", [((128, 256), 8100, 20, 2048, 576),
+                                          ((256, 256), 17000, 4, 2048, 640)])
+def test_rows_left_and_one_expert_with_all(tile, T, E, N, K, act):
+    """The large tiles where one expert has nearly every row, another one row, others none;
+    rows behind the last expert and of an expert without a slot keep what they held."""
+    case(f"mx4 product: one expert, rows left, tile={tile} act={act}")
+    assert laep.laep_mx4_product_tile(T, E, N, K, act) == tile
+    g = np.random.default_rng(T)
+    sizes = np.zeros(E, np.int64)
+    sizes[1], sizes[3] = 1, 300
+    sizes[2] = T - 7 - 301
+    offsets = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)
+    emap = np.full(E, -1, np.int32)
+    emap[1], emap[2] = 1, 0
+    row_src = g.permutation(T).astype(np.int32)
+    x = round_bf16(g.normal(size=(T, K)))
+    qw, qx = mx4.quantize(g.normal(size=(2, N, K))), mx4.quantize(x)
+    xv = mx4.dequantize(*qx) if act == 4 else x
+    ref, mag = mx4.grouped_product(xv[row_src], mx4.dequantize(*qw), offsets, emap)
+    out = torch.full((T, N), 7.0, dtype=torch.float32, device="cuda")
+    laep.moe_mx4_grouped_product(_mx4(qx) if act == 4 else dev(x, torch.bfloat16), _mx4(qw),
+                                 _i32(offsets), row_src=_i32(row_src), k=1, expert_map=_i32(emap),
+                                 dtype=torch.float32, out=out)
+    live = int(offsets[3])
+    got = host(out)
+    assert (np.abs(got - ref)[:live] <= _bound(mag, ref, K, "f32")[:live]).all()
+    assert (got[live:] == 7.0).all()
