@@ -149,9 +149,9 @@ __device__ __forceinline__ void grouped_tile(int i, int mt, int n_tiles, int gro
 // (E <= 256, one LDS scan) and writes the tiles of its own range of the list,
 // finding each tile's expert by binary search over the starts.  Launch with
 // enough workgroups to cover the larger list's max_entries.
-__device__ __forceinline__ void build_tile_lists(
-    int block, const int32_t* __restrict__ offsets, const int32_t* __restrict__ expert_map, int E,
-    int BM, const TileList& la, const TileList& lb) {
+__global__ __launch_bounds__(kTableThreads) void build_tile_lists_kernel(
+    const int32_t* __restrict__ offsets, const int32_t* __restrict__ expert_map, int E, int BM,
+    TileList la, TileList lb) {
   __shared__ int s_tmp[4];
   __shared__ int s_start[kTableThreads + 1];
   __shared__ int s_mt[kTableThreads];
@@ -177,11 +177,11 @@ __device__ __forceinline__ void build_tile_lists(
     if (e == kTableThreads - 1) s_start[kTableThreads] = start + cnt;
     __syncthreads();
     const int total = s_start[kTableThreads];
-    if (block == 0 && e == 0) *L.n_entries = min(total, L.max_entries);
+    if (blockIdx.x == 0 && e == 0) *L.n_entries = min(total, L.max_entries);
     // the persistent products' per-XCD tile counters (kTileCtrOffset ints into
     // the table header), zeroed for the launch that follows on the stream
-    if (block == 0 && e < 8) L.n_entries[kTileCtrOffset + e] = 0;
-    const int i = block * kTableThreads + e;
+    if (blockIdx.x == 0 && e < 8) L.n_entries[kTileCtrOffset + e] = 0;
+    const int i = blockIdx.x * kTableThreads + e;
     if (i < total && i < L.max_entries) {
       int lo = 0, hi = kTableThreads - 1;  // last expert with start <= i
       while (lo < hi) {
@@ -202,12 +202,6 @@ __device__ __forceinline__ void build_tile_lists(
     }
     __syncthreads();  // s_start is rewritten for the second list
   }
-}
-
-__global__ __launch_bounds__(kTableThreads) void build_tile_lists_kernel(
-    const int32_t* __restrict__ offsets, const int32_t* __restrict__ expert_map, int E, int BM,
-    TileList la, TileList lb) {
-  build_tile_lists(blockIdx.x, offsets, expert_map, E, BM, la, lb);
 }
 
 struct FoundTile : TileEntry {
