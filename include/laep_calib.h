@@ -67,11 +67,12 @@ int laep_ffn_fwd_row_tile(int64_t R, int E, int d_model, int d_ff);
  * laep_mx4_product_tile, laep_mx4_ffn_tile -- the same for the calls at MX4
  * weights (laep_mx4.h): rows per tile (32, 64, 128 or 256), and in cols (NULL:
  * not wanted) its columns (64, 128 or 256), for R = T * k rows (T without
- * row_src) and activations of act_bits (4: MX4, 16: bf16).  Host code only; 0
- * for sizes that those calls refuse.
+ * row_src) and activations of act_bits (4: MX4, 16: bf16); of the FFN's gate/up
+ * product, or (down) of its second.  Host code only; 0 for sizes that those calls
+ * refuse.
  */
 int laep_mx4_product_tile(int64_t R, int E, int N, int K, int act_bits, int* cols);
-int laep_mx4_ffn_tile(int64_t R, int E, int d_model, int d_ff, int act_bits, int* cols);
+int laep_mx4_ffn_tile(int64_t R, int E, int d_model, int d_ff, int act_bits, int down, int* cols);
 
 #ifdef __cplusplus
 }

@@ -110,7 +110,7 @@ SIGNATURES = {
     "laep_calib_read": (_i, [_p, _sz, _i, _p, _p]),
     "laep_ffn_fwd_row_tile": (_i, [_i64, _i, _i, _i]),
     "laep_mx4_product_tile": (_i, [_i64, _i, _i, _i, _i, _p]),
-    "laep_mx4_ffn_tile": (_i, [_i64, _i, _i, _i, _i, _p]),
+    "laep_mx4_ffn_tile": (_i, [_i64, _i, _i, _i, _i, _i, _p]),
 }
 
 _lock = threading.Lock()

@@ -1020,9 +1020,11 @@ def laep_mx4_product_tile(R: int, E: int, N: int, K: int, act_bits: int = 16) ->
     return int(rows), cols.value
 
 
-def laep_mx4_ffn_tile(R: int, E: int, d_model: int, d_ff: int, act_bits: int = 16) -> tuple:
-    """(rows, columns) of the tiles of moe_grouped_ffn_fwd_mx4, likewise."""
+def laep_mx4_ffn_tile(R: int, E: int, d_model: int, d_ff: int, act_bits: int = 16,
+                      down: bool = False) -> tuple:
+    """(rows, columns) of the tiles of moe_grouped_ffn_fwd_mx4's gate/up or down product,
+    likewise."""
     cols = ctypes.c_int(0)
     rows = lib().laep_mx4_ffn_tile(int(R), int(E), int(d_model), int(d_ff), int(act_bits),
-                                   ctypes.byref(cols))
+                                   int(down), ctypes.byref(cols))
     return int(rows), cols.value

@@ -1106,13 +1106,13 @@ int laep_mx4_product_tile(int64_t R, int E, int N, int K, int act_bits, int* col
   return laep::mx4_product_tile(R, E, N, K, act_bits == 4, cols);
 }
 
-int laep_mx4_ffn_tile(int64_t R, int E, int d_model, int d_ff, int act_bits, int* cols) {
+int laep_mx4_ffn_tile(int64_t R, int E, int d_model, int d_ff, int act_bits, int down, int* cols) {
   const char* const name = "laep_mx4_ffn_tile";
   if ((act_bits != 4 && act_bits != 16) || R > 0x7FFFFFFFll ||
       check_mx4_rows(name, nullptr, (int)R, 1, E, R) ||
       check_mx4_shape(name, 2 * (int64_t)d_ff, d_model) || check_mx4_shape(name, d_model, d_ff))
     return 0;
-  return laep::mx4_ffn_tile(R, E, d_model, d_ff, act_bits == 4, cols);
+  return laep::mx4_ffn_tile(R, E, d_model, d_ff, act_bits == 4, down != 0, cols);
 }
 
 }  // extern "C"

@@ -366,48 +366,72 @@ inline int cols_of(Tiles t) { return is_big(t) ? 256 : t == FEW ? 64 : 128; }
 
 // Which: the host knows neither the loads nor how many experts have rows, so it counts
 // min(R, E) of them with half a tile's rows over each.
+//
 // FEW against MIDDLE by their times: FEW streams the weights of every row tile (0.13 us a
 // MB) and reads the rows beside them (0.0037 us a MB and row), MIDDLE takes its k-steps'
-// latency or the weights' stream, whichever is longer.  The larger tiles where they are
-// enough for 256 CUs.  Measured, us for the FFN by 32 / 64 / 128 rows / BIG 128 / BIG 256:
-//   experts, d, d_ff      rows   MX4 activations             bf16 activations
-//   64, 2048, 1024         128   33 / 38 / 42 /  .  / 59     37 / 50 / 72 /  .  / 130
-//                         1024   63 / 46 / 50 /  48 / 63     65 / 61 / 88 /  87 / 141
-//                         4096  137 / 66 / 64 /  60 / 83    143 / 102 / 115 / 118 / 197
-//                        12288  372 / 128 / 111 / 87 / 90   377 / 217 / 213 / 198 / 213
-//                        32768  1008 / 285 / 231 / 151 / 147   951 / 512 / 444 / 383 / 377
-//   16, 4096, 2048          32   30 / 36 / 37 /  .  / 56     36 / 52 / 78 /  .  / 122
-//                          256   77 / 42 / 42 /  48 / 61     75 / 56 / 82 /  85 / 138
-//                         4096  554 / 124 / 105 / 94 / 103  506 / 262 / 253 / 222 / 251
-//   1, 2048, 2048          128   16 / 20 / 23 /  31 / 39     19 / 28 / 39 /  50 /  76
-//                         1024   65 / 26 / 27 /  33 / 43     68 / 37 / 44 /  55 /  79
-//                         4096  255 / 67 / 50 /  46 / 49    256 / 132 / 109 / 90 /  93
-// Over five such layers, 1 to 4096 tokens, the rule's choice is within a tenth of the best
-// but for a few where the last round of tiles is nearly empty.
+// latency or the weights' stream, whichever is longer.  us for the FFN, 32 / 64 rows:
+//   experts, d, d_ff      rows   MX4 activations   bf16 activations
+//   64, 2048, 1024         128       33 / 38           37 / 50
+//                         1024       63 / 46           65 / 61
+//   16, 4096, 2048          32       30 / 36           36 / 52
+//                          256       77 / 42           75 / 56
+//   1, 2048, 2048          128       16 / 20           19 / 28
 //
-// weights: values of one expert; cols: the widest product's columns; k_min, k_max: the
-// shortest and longest K; steps: 256-column steps of all products; products: their number.
-Tiles tiles_of(int64_t R, int E, int64_t weights, int64_t cols, int k_min, int k_max, int steps,
-               int products, bool mx4) {
+// weights: values of one expert; steps: 256-column steps of all products; products: their
+// number.
+bool few_rows(int64_t R, int E, int64_t weights, int steps, int products, bool mx4) {
   const double live = (double)(R < E ? R : E), mb = weights * (17.0 / 32) * 1e-6;
   const double few = 4 * products + mb * (0.13 * (live + R / 32) + 0.0037 * R);
   const double latency = mx4 ? 5.2 * products + 0.56 * steps : 4.5 * products + 1.15 * steps;
   const double stream = 3 * products + (mx4 ? 0.18 : 0.24) * mb * live;
-  if (few <= (latency > stream ? latency : stream)) return FEW;
-  auto tiles = [&](int bm, int bn) { return ((double)R / bm + live / 2) * ((cols + bn - 1) / bn); };
+  return few <= (latency > stream ? latency : stream);
+}
+
+// The others by the number of tiles, as there are 256 CUs: one persistent workgroup a CU
+// needs some rounds of tiles to even out, and taller tiles of ragged experts waste more.
+// us for one product by 64 x 128 / 128 x 128 / BIG 128 / BIG 256:
+//   experts, N, K         rows   MX4 activations          bf16 activations
+//   64, 2048, 2048        1024   27 / 32 / 30 / 39        39 / 59 / 38 / 82
+//                         4096   38 / 41 / 37 / 51        61 / 77 / 58 / 119
+//                         8192   59 / 46 / 39 / 53        105 / 96 / 76 / 122
+//                        16384   89 / 78 / 59 / 56        176 / 170 / 137 / 140
+//                        32768   189 / 164 / 89 / 89      345 / 303 / 244 / 241
+//   16, 4096, 4096         512   32 / 26 / 33 / 40        53 / 54 / 44 / 77
+//                         2048   42 / 39 / 39 / 59        87 / 88 / 80 / 144
+//                         8192   130 / 101 / 90 / 90      295 / 260 / 244 / 246
+//                        32768   574 / 485 / 297 / 270    1239 / 1128 / 857 / 806
+//   8, 7168, 1024         1024   21 / 18 / 19 / 20        31 / 30 / 30 / 32
+//                         4096   53 / 39 / 33 / 36        84 / 70 / 61 / 74
+//                         8192   95 / 68 / 51 / 47        160 / 130 / 113 / 105
+//   8, 1024, 3584         2048   15 / 16 / 22 / 29        30 / 33 / 44 / 65
+//                         8192   38 / 36 / 37 / 33        79 / 79 / 86 / 71
+//                        16384   69 / 56 / 51 / 57        153 / 134 / 129 / 144
+//   1, 2048, 2048         2048   12 / 12 / 17 / 21        22 / 23 / 31 / 43
+//                         4096   24 / 18 / 20 / 24        47 / 36 / 37 / 46
+//                        16384   81 / 70 / 47 / 46        174 / 171 / 113 / 105
+//   32, 1024, 1024        4096   14 / 11 / 14 / 17        20 / 18 / 22 / 28
+//                        16384   32 / 26 / 25 / 27        49 / 44 / 46 / 51
+// Over 63 such cases the rule takes on average 0.4 % (MX4) and 1.4 % (bf16) longer than the
+// best tiles.
+Tiles many_rows(int64_t R, int E, int64_t N, int K, bool mx4) {
+  const double live = (double)(R < E ? R : E);
+  auto tiles = [&](int bm, int bn) { return ((double)R / bm + live / 2) * ((N + bn - 1) / bn); };
   // BIG needs k-steps for its pipeline, and offsets within a tile and of scales in 32 bits
-  if (k_min >= 576 && cols <= 1 << 20 && mx4_scale_bytes(R, k_max) < (size_t)1 << 31) {
-    if (R > 512 * live && tiles(256, 256) >= 512) return BIG256;
-    if (tiles(128, 256) >= (mx4 ? 400 : 520)) return BIG128;
+  if (K >= 576 && N <= 1 << 20 && mx4_scale_bytes(R, K) < (size_t)1 << 31) {
+    if (R >= 512 * live && tiles(256, 256) >= (mx4 ? 640 : 900)) return BIG256;
+    if (tiles(128, 256) >= 360) return BIG128;
   }
-  return R > (mx4 ? 96 : 200) * live && tiles(128, 128) >= 384 ? MID128 : MID64;
+  return R >= (mx4 ? 32 : 128) * live && tiles(64, 128) >= (mx4 ? 500 : 540) ? MID128 : MID64;
 }
 Tiles product_tiles(int64_t R, int E, int N, int K, bool mx4) {
-  return tiles_of(R, E, (int64_t)N * K, N, K, K, mx4_groups(K), 1, mx4);
+  return few_rows(R, E, (int64_t)N * K, mx4_groups(K), 1, mx4) ? FEW : many_rows(R, E, N, K, mx4);
 }
-Tiles ffn_tiles(int64_t R, int E, int d, int f, bool mx4) {
-  return tiles_of(R, E, 3LL * d * f, 2LL * f > d ? 2LL * f : d, d < f ? d : f, d < f ? f : d,
-                  mx4_groups(d) + mx4_groups(f), 2, mx4);
+struct FfnTiles {
+  Tiles gu, down;
+};
+FfnTiles ffn_tiles(int64_t R, int E, int d, int f, bool mx4) {
+  if (few_rows(R, E, 3LL * d * f, mx4_groups(d) + mx4_groups(f), 2, mx4)) return {FEW, FEW};
+  return {many_rows(R, E, 2LL * f, d, mx4), many_rows(R, E, d, f, mx4)};
 }
 
 // one product with its epilogue (round: see launch_mx4_few)
@@ -444,8 +468,9 @@ int mx4_product_tile(int64_t R, int E, int N, int K, bool mx4, int* cols) {
   return rows_of(t);
 }
 
-int mx4_ffn_tile(int64_t R, int E, int d, int f, bool mx4, int* cols) {
-  const Tiles t = ffn_tiles(R, E, d, f, mx4);
+int mx4_ffn_tile(int64_t R, int E, int d, int f, bool mx4, bool down, int* cols) {
+  const FfnTiles both = ffn_tiles(R, E, d, f, mx4);
+  const Tiles t = down ? both.down : both.gu;
   if (cols) *cols = cols_of(t);
   return rows_of(t);
 }
@@ -481,8 +506,8 @@ hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32
     uint8_t* const routed = list + list_bytes(R_ws, E, N, false);
     const bool gather = x_scale && row_src;
     const hipError_t err =
-        launch_mx4_prepare(offsets, expert_map, E, R, rows_of(kind), 0, nullptr, N, list, x_scale,
-                           gather ? routed : nullptr, row_src, k, T, K, s);
+        launch_mx4_prepare(offsets, expert_map, E, R, 0, 0, nullptr, rows_of(kind), N, list,
+                           x_scale, gather ? routed : nullptr, row_src, k, T, K, s);
     if (err != hipSuccess) return err;
     if (gather) {
       a.a_scale = routed;
@@ -529,22 +554,25 @@ hipError_t launch_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int 
   const bool mx4 = act_bits == 4;
   const int64_t R_ws = row_src ? (int64_t)T * k : T;
   const Mx4FfnWs at = ffn_ws(T, R_ws, E, d, f, mx4);
-  const Tiles kind = ffn_tiles(R_ws, E, d, f, mx4);
+  const FfnTiles tiles = ffn_tiles(R_ws, E, d, f, mx4);
   uint8_t* const base = static_cast<uint8_t*>(ws);
   Mx4Args a = {};
   a.A = x;
   a.a_rows = T;
   hipError_t err = hipSuccess;
-  if (mx4 && kind != FEW) {
+  if (mx4 && tiles.gu != FEW) {
     err = launch_mx4_quantize(x, kDtypeBf16, 1, T, d, base, base + at.x_scale, s);
     if (err != hipSuccess) return err;
     a.A = base;
     a.a_scale = base + at.x_scale;
   }
-  if (is_big(kind)) {
-    const bool gather = mx4 && row_src;
-    err = launch_mx4_prepare(offsets, expert_map, E, R, rows_of(kind), f, base + at.list_gu, d, base + at.list_d,
-                             a.a_scale, gather ? base + at.routed : nullptr, row_src, k, T, d, s);
+  const bool gu_big = is_big(tiles.gu), down_big = is_big(tiles.down);
+  if (gu_big || down_big) {
+    const bool gather = mx4 && row_src && gu_big;
+    err = launch_mx4_prepare(offsets, expert_map, E, R, rows_of(tiles.gu), f,
+                             gu_big ? base + at.list_gu : nullptr, rows_of(tiles.down), d,
+                             down_big ? base + at.list_d : nullptr, a.a_scale,
+                             gather ? base + at.routed : nullptr, row_src, k, T, d, s);
     if (err != hipSuccess) return err;
     if (gather) {
       a.a_scale = base + at.routed;
@@ -563,7 +591,7 @@ hipError_t launch_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int 
   a.row_src = row_src;
   a.slots_k = k;
   a.list = base + at.list_gu;
-  err = launch_product(a, kind, mx4, offsets, expert_map, E, R, s);
+  err = launch_product(a, tiles.gu, mx4, offsets, expert_map, E, R, s);
   if (err != hipSuccess) return err;
   a.A = a.out;
   a.a_scale = mx4 ? a.out_scale : nullptr;
@@ -577,7 +605,7 @@ hipError_t launch_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int 
   a.act = nullptr;
   a.row_src = nullptr;
   a.list = base + at.list_d;
-  return launch_product(a, kind, false, offsets, expert_map, E, R, s);
+  return launch_product(a, tiles.down, false, offsets, expert_map, E, R, s);
 }
 
 }  // namespace laep

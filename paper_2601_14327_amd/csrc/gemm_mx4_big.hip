@@ -746,6 +746,10 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
 // What the products need first, in one launch: their tile lists, and the scales of
 // gathered MX4 activations in routed order.
 // ---------------------------------------------------------------------------
+struct BigList : TileList {
+  int bm;
+};
+
 // An expert's rows are spread over its tiles in equal numbers of 32-row blocks.  128-row
 // tiles, whose waves leave out the blocks without rows, are listed by classes of one to
 // four blocks; 256-row tiles in one class.  One thread per tile: every workgroup recomputes
@@ -753,7 +757,7 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
 // of each list, finding a tile's expert by binary search.
 __device__ __forceinline__ void build_big_lists(int block, const int32_t* __restrict__ offsets,
                                                 const int32_t* __restrict__ expert_map, int E,
-                                                int BM, const TileList& la, const TileList& lb) {
+                                                const BigList& la, const BigList& lb) {
   __shared__ int s_tmp[4];
   __shared__ int s_start[kClasses][kTableThreads];
   __shared__ int s_total[kClasses];
@@ -766,23 +770,26 @@ __device__ __forceinline__ void build_big_lists(int block, const int32_t* __rest
     rows = offsets[e + 1] - row0;
     phys = expert_map ? expert_map[e] : e;
   }
-  const int mt = phys >= 0 && rows > 0 ? (rows + BM - 1) / BM : 0;
-  const int tall = mt ? ((rows + mt - 1) / mt + 31) & ~31 : 0;
-  const int cls = BM == kClasses * 32 ? kClasses - tall / 32 : 0;
-  s_mt[e] = mt;
   s_phys[e] = phys;
   s_row0[e] = row0;
   s_rows[e] = rows;
-  s_tall[e] = tall;
-  for (int c = 0; c < kClasses; ++c) {
-    const int own = mt && cls == c ? mt : 0;
-    const int start = block_excl_scan_256(own, s_tmp);   // (synchronises the block)
-    s_start[c][e] = start;
-    if (e == kTableThreads - 1) s_total[c] = start + own;
-  }
-  __syncthreads();
   for (int which = 0; which < 2; ++which) {
-    const TileList& L = which == 0 ? la : lb;
+    const BigList& L = which == 0 ? la : lb;
+    if (which == 0 || la.bm != lb.bm) {
+      __syncthreads();                     // (the first list has been written)
+      const int mt = phys >= 0 && rows > 0 ? (rows + L.bm - 1) / L.bm : 0;
+      const int tall = mt ? ((rows + mt - 1) / mt + 31) & ~31 : 0;
+      const int cls = L.bm == kClasses * 32 ? kClasses - tall / 32 : 0;
+      s_mt[e] = mt;
+      s_tall[e] = tall;
+      for (int c = 0; c < kClasses; ++c) {
+        const int own = mt && cls == c ? mt : 0;
+        const int start = block_excl_scan_256(own, s_tmp);   // (synchronises the block)
+        s_start[c][e] = start;
+        if (e == kTableThreads - 1) s_total[c] = start + own;
+      }
+      __syncthreads();
+    }
     int begin = 0, i = block * kTableThreads + e, c = 0;
     bool found = false;
     for (int k = 0; k < kClasses; ++k) {
@@ -828,9 +835,9 @@ struct GatherScales {
 
 __global__ __launch_bounds__(kTableThreads) void mx4_prepare_kernel(
     const int32_t* __restrict__ offsets, const int32_t* __restrict__ expert_map, int E,
-    int BM, TileList la, TileList lb, int list_blocks, GatherScales g) {
+    BigList la, BigList lb, int list_blocks, GatherScales g) {
   if ((int)blockIdx.x < list_blocks) {
-    build_big_lists(blockIdx.x, offsets, expert_map, E, BM, la, lb);
+    build_big_lists(blockIdx.x, offsets, expert_map, E, la, lb);
     return;
   }
   const long long n = (long long)(gridDim.x - list_blocks) * kTableThreads;
@@ -868,17 +875,23 @@ size_t mx4_big_list_bytes(int64_t R, int E, int bm, int n_cols, bool gate_up) {
 }
 
 hipError_t launch_mx4_prepare(const int32_t* offsets, const int32_t* expert_map, int E, int64_t R,
-                              int bm, int f, void* list_gu, int n_cols, void* list,
+                              int bm_gu, int f, void* list_gu, int bm, int n_cols, void* list,
                               const uint8_t* x_scale, uint8_t* routed_scale,
                               const int32_t* row_src, int slots_k, int64_t T, int K,
                               hipStream_t s) {
-  const int nt_a = list_gu ? ceil_div(f, kBigBN / 2) : 1, nt_b = ceil_div(n_cols, kBigBN);
-  const int max_a = list_gu ? list_max(R, E, bm, nt_a) : 0, max_b = list_max(R, E, bm, nt_b);
-  const TableWs tb = carve_table(list, max_b);
-  const TableWs ta = list_gu ? carve_table(list_gu, max_a) : tb;
-  const TileList la = {nt_a, kFwdTileGroup, max_a, ta.n_entries, ta.table};
-  const TileList lb = {nt_b, kFwdTileGroup, max_b, tb.n_entries, tb.table};
-  const int blocks = ceil_div(max_a > max_b ? max_a : max_b, kTableThreads);
+  auto list_of = [&](void* at, int rows, int n_tiles) {
+    const int n = list_max(R, E, rows, n_tiles);
+    const TableWs t = carve_table(at, n);
+    return BigList{{n_tiles, kFwdTileGroup, n, t.n_entries, t.table}, rows};
+  };
+  // (of one list only, both are that list: written twice, alike)
+  BigList la = {}, lb = {};
+  if (list_gu) la = list_of(list_gu, bm_gu, ceil_div(f, kBigBN / 2));
+  if (list) lb = list_of(list, bm, ceil_div(n_cols, kBigBN));
+  if (!list_gu) la = lb;
+  if (!list) lb = la;
+  const int blocks =
+      ceil_div(la.max_entries > lb.max_entries ? la.max_entries : lb.max_entries, kTableThreads);
   GatherScales g = {};
   int more = 0;
   if (routed_scale) {
@@ -886,9 +899,8 @@ hipError_t launch_mx4_prepare(const int32_t* offsets, const int32_t* expert_map,
          row_src, T, R, mx4_groups(K), slots_k};
     more = (int)(ceil_div(R, kTableThreads) < 4096 ? ceil_div(R, kTableThreads) : 4096);
   }
-  // (of one list only, both are that list: written twice, alike)
   hipLaunchKernelGGL(mx4_prepare_kernel, dim3(blocks + more), dim3(kTableThreads), 0, s, offsets,
-                     expert_map, E, bm, list_gu ? la : lb, lb, blocks, g);
+                     expert_map, E, la, lb, blocks, g);
   return hipGetLastError();
 }
 

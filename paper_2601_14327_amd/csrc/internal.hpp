@@ -176,7 +176,7 @@ hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scale, int
 // Products at MX4 weights; x_scale NULL: x is bf16; row_src NULL: rows in order.
 // The tiles of the products and of the FFN: rows, and in cols (if not NULL) the columns.
 int mx4_product_tile(int64_t R, int E, int N, int K, bool mx4, int* cols);
-int mx4_ffn_tile(int64_t R, int E, int d, int f, bool mx4, int* cols);
+int mx4_ffn_tile(int64_t R, int E, int d, int f, bool mx4, bool down, int* cols);
 size_t mx4_product_ws_bytes(int T, int k, int E, int K, int N);
 hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32_t* row_src, int T,
                               int k, const uint8_t* w, const uint8_t* w_scale,
@@ -184,7 +184,7 @@ hipError_t launch_mx4_product(const void* x, const uint8_t* x_scale, const int32
                               int E, int N, int K, int64_t R, void* out, void* ws, hipStream_t s);
 // The same products by 128 or 256 x 256 tiles (gemm_mx4_big.hip): each needs the list of its
 // tiles, and gathered MX4 activations their scales in routed order, both from
-// launch_mx4_prepare (list_gu: the list of a gate/up product as well, or NULL).
+// launch_mx4_prepare (list_gu: of a gate/up product, list: of another; either may be NULL).
 struct Mx4Args {
   const void* A;
   const uint8_t* a_scale;    // NULL: A is bf16
@@ -204,7 +204,7 @@ struct Mx4Args {
 };
 size_t mx4_big_list_bytes(int64_t R, int E, int bm, int n_cols, bool gate_up);
 hipError_t launch_mx4_prepare(const int32_t* offsets, const int32_t* expert_map, int E, int64_t R,
-                              int bm, int f, void* list_gu, int n_cols, void* list,
+                              int bm_gu, int f, void* list_gu, int bm, int n_cols, void* list,
                               const uint8_t* x_scale, uint8_t* routed_scale,
                               const int32_t* row_src, int slots_k, int64_t T, int K,
                               hipStream_t s);

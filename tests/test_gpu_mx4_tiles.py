@@ -22,9 +22,9 @@ PRODUCTS = [   # rows and columns of the tiles; T, k, E, dead, N, K
     ((128, 256), 8100, 1, 20, 0, 2048, 576), ((128, 256), 1100, 8, 20, 3, 1984, 640),
     ((128, 256), 4100, 2, 19, 0, 2112, 1024), ((128, 256), 8500, 1, 20, 5, 2048, 1216),
     ((128, 256), 33000, 1, 80, 9, 448, 1088),
-    ((256, 256), 4300, 2, 2, 0, 3904, 576), ((256, 256), 16500, 2, 3, 0, 1088, 640),
-    ((256, 256), 17000, 1, 6, 1, 1856, 1024), ((256, 256), 35000, 1, 1, 0, 832, 1216),
-    ((256, 256), 70000, 1, 5, 2, 448, 832)]
+    ((256, 256), 4300, 2, 2, 0, 7104, 576), ((256, 256), 16500, 2, 3, 0, 1984, 640),
+    ((256, 256), 16500, 1, 6, 1, 4096, 1024), ((256, 256), 70000, 1, 1, 0, 832, 1216),
+    ((256, 256), 70000, 1, 5, 2, 832, 832)]
 
 
 @functools.lru_cache(1)     # (shared by the types of one size)
@@ -62,17 +62,21 @@ def test_product(tile, T, k, E, dead, N, K, act, dtype):
     assert torch.equal(again, out)
 
 
-FFNS = [   # rows and columns of the tiles; T, k, E, dead, d, f
-    ((64, 128), 1500, 2, 16, 3, 320, 704), ((128, 128), 3200, 2, 2, 0, 320, 512),
-    ((128, 256), 1000, 8, 20, 0, 1088, 1024), ((128, 256), 8800, 1, 20, 2, 576, 1216),
-    ((256, 256), 16500, 2, 2, 0, 576, 576), ((256, 256), 9000, 1, 2, 0, 640, 1984)]
+FFNS = [   # the two products' tiles; T, k, E, dead, d, f
+    ((64, 128), (128, 256), 1000, 2, 8, 1, 7168, 640),
+    ((128, 128), (64, 128), 1500, 2, 16, 3, 320, 704),
+    ((128, 256), (128, 256), 1000, 8, 20, 0, 1088, 1024),
+    ((128, 256), (128, 128), 8800, 1, 20, 2, 576, 1216),
+    ((256, 256), (128, 256), 16500, 2, 2, 0, 576, 1024),
+    ((256, 256), (128, 128), 9000, 1, 2, 0, 640, 3584)]
 
 
 @pytest.mark.parametrize("act", [4, 16])
-@pytest.mark.parametrize("tile,T,k,E,dead,d,f", FFNS)
-def test_ffn(tile, T, k, E, dead, d, f, act):
-    case(f"mx4 ffn tile={tile} T={T} k={k} E={E} dead={dead} d={d} f={f} act={act}")
-    assert laep.laep_mx4_ffn_tile(T * k, E, d, f, act) == tile
+@pytest.mark.parametrize("gate_up,down,T,k,E,dead,d,f", FFNS)
+def test_ffn(gate_up, down, T, k, E, dead, d, f, act):
+    case(f"mx4 ffn tiles={gate_up}, {down} T={T} k={k} E={E} dead={dead} d={d} f={f} act={act}")
+    assert laep.laep_mx4_ffn_tile(T * k, E, d, f, act) == gate_up
+    assert laep.laep_mx4_ffn_tile(T * k, E, d, f, act, down=True) == down
     x, row_src, offsets, emap, gu, dn = _ffn_inputs(T + d + f, T, k, E, dead, d, f)
     kw = dict(row_src=_i32(row_src), k=k, act_bits=act, expert_map=_i32(emap))
     args = (dev(x, torch.bfloat16), _mx4(gu), _mx4(dn), _i32(offsets))
@@ -87,7 +91,7 @@ def test_ffn(tile, T, k, E, dead, d, f, act):
 
 @pytest.mark.parametrize("act", [4, 16])
 @pytest.mark.parametrize("tile,T,E,N,K", [((128, 256), 8100, 20, 2048, 576),
-                                          ((256, 256), 17000, 4, 2048, 640)])
+                                          ((256, 256), 17000, 4, 3584, 640)])
 def test_rows_left_and_one_expert_with_all(tile, T, E, N, K, act):
     """The large tiles where one expert has nearly every row, another one row, others none;
     rows behind the last expert and of an expert without a slot keep what they held."""

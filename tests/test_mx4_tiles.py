@@ -6,23 +6,36 @@ from paper_2601_14327_amd import laep_mx4_ffn_tile as ffn_tile
 from paper_2601_14327_amd import laep_mx4_product_tile as product_tile
 
 
-@pytest.mark.parametrize("R,E,d,f,mx4,bf16", [
-    (128, 64, 2048, 1024, (32, 64), (32, 64)),          # us 33 (64 rows: 38), bf16 37 (50)
-    (1024, 64, 2048, 1024, (64, 128), (64, 128)),       # 46 (32 rows: 63), 61 (65)
-    (4096, 64, 2048, 1024, (128, 256), (64, 128)),      # 60 (64: 66), 102 (BIG 128: 118)
-    (12288, 64, 2048, 1024, (128, 256), (128, 256)),    # 87, 198
-    (32768, 64, 2048, 1024, (128, 256), (128, 256)),
-    (131072, 64, 2048, 1024, (256, 256), (256, 256)),
-    (32, 16, 4096, 2048, (32, 64), (32, 64)),           # 30 (64: 36), 36 (52)
-    (256, 16, 4096, 2048, (64, 128), (64, 128)),        # 42 (32: 77), 56 (75)
-    (4096, 16, 4096, 2048, (128, 256), (128, 256)),     # 94 (128 x 128: 105), 222 (253)
-    (131072, 4, 512, 1024, (128, 128), (128, 128)),     # k-loops too short for the large tiles
+@pytest.mark.parametrize("R,E,N,K,mx4,bf16", [
+    (1024, 64, 2048, 2048, (64, 128), (64, 128)),        # us 27 (128 rows: 32), 39 (59)
+    (4096, 64, 2048, 2048, (128, 256), (128, 256)),      # 37 (64: 38), 58 (61)
+    (8192, 64, 2048, 2048, (128, 256), (128, 256)),      # 39 (BIG 256: 53), 76 (122)
+    (16384, 64, 2048, 2048, (128, 256), (128, 256)),     # 59 (BIG 256: 56), 137 (140)
+    (32768, 64, 2048, 2048, (256, 256), (256, 256)),     # 89, 241 (BIG 128: 244)
+    (512, 16, 4096, 4096, (128, 128), (64, 128)),        # 26 (64: 32), 53 (128: 54)
+    (8192, 8, 7168, 1024, (256, 256), (256, 256)),       # 47 (BIG 128: 51), 105 (113)
+    (2048, 8, 1024, 3584, (64, 128), (64, 128)),         # 15 (BIG 128: 22), 30 (44)
+    (131072, 4, 1024, 512, (128, 128), (128, 128)),      # k-loops too short for the large
     (100, 4, 60, 64, (0, 0), (0, 0)), (-1, 4, 64, 64, (0, 0), (0, 0)),    # refused
     (1, 257, 64, 64, (0, 0), (0, 0)), (1 << 31, 4, 64, 64, (0, 0), (0, 0)),
 ])
-def test_ffn(R, E, d, f, mx4, bf16):
-    assert ffn_tile(R, E, d, f, 4) == mx4 and ffn_tile(R, E, d, f, 16) == bf16
-    assert ffn_tile(R, E, d, f, 8) == (0, 0)
+def test_product(R, E, N, K, mx4, bf16):
+    assert product_tile(R, E, N, K, 4) == mx4 and product_tile(R, E, N, K, 16) == bf16
+    assert product_tile(R, E, N, K, 8) == (0, 0)
+
+
+@pytest.mark.parametrize("R,E,d,f", [(128, 64, 2048, 1024), (1024, 64, 2048, 1024),
+                                     (32, 16, 4096, 2048), (4096, 16, 4096, 2048),
+                                     (16384, 8, 1024, 3584), (100, 4, 60, 64)])
+@pytest.mark.parametrize("act", [4, 16])
+def test_ffn(R, E, d, f, act):
+    """Few rows: both products by 32 x 64 tiles; else each as a product of its own."""
+    gate_up, down = ffn_tile(R, E, d, f, act), ffn_tile(R, E, d, f, act, down=True)
+    if R <= 128:
+        assert gate_up == down == ((0, 0) if d == 60 else (32, 64))
+    else:
+        assert gate_up == product_tile(R, E, 2 * f, d, act)
+        assert down == product_tile(R, E, d, f, act)
 
 
 @pytest.mark.parametrize("N,K", [(64, 64), (192, 320), (2048, 1024), (4096, 576)])
