@@ -411,7 +411,7 @@ bool few_rows(int64_t R, int E, int64_t weights, int steps, int products, bool m
 //                        16384   81 / 70 / 47 / 46        174 / 171 / 113 / 105
 //   32, 1024, 1024        4096   14 / 11 / 14 / 17        20 / 18 / 22 / 28
 //                        16384   32 / 26 / 25 / 27        49 / 44 / 46 / 51
-// Over 63 such cases the rule takes on average 0.4 % (MX4) and 1.4 % (bf16) longer than the
+// Over 63 such cases the rule takes on average 0.6 % (MX4) and 1.4 % (bf16) longer than the
 // best tiles.
 Tiles many_rows(int64_t R, int E, int64_t N, int K, bool mx4) {
   const double live = (double)(R < E ? R : E);

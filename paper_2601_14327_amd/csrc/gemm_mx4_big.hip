@@ -1,17 +1,31 @@
 // Grouped products at MX4 weights for many rows: the products of gemm_mx4.hip in tiles of
-// 256 x 256, one persistent workgroup of eight waves (2 x 4, each 128 x 64) a CU.
+// 256 or 128 x 256, one persistent workgroup of eight waves (2 x 4, each 128 or 64 x 64) a
+// CU.
 //
-// The k-steps of all the tiles that a workgroup walks are one stream: copies run two
-// steps (three for bf16 activations) ahead of the matrix instructions, past a tile's end
-// into the next tile, whose token rows were read a tile earlier, and so do the reads of
-// fragments.  A tile's epilogue, from registers to memory, lies between two steps with
-// the next tile's operands landed or in flight.
-//   MX4:  a step is 256 columns, 32 KB ("half") of each operand; the LDS is a ring of
-//         five halves (A0 B0 A1 B1 A2 | B2 A3 ...).  Scales go straight to registers, one
-//         dword per fragment and step; those of gathered activations lie in routed order
-//         (a scale of a gathered row would cost a cache line a step, as much as its codes).
-//   bf16: a step is 64 columns, 32 KB of activations and 8 KB of weight codes; the LDS
-//         is a ring of four.
+// The k-steps of all the tiles that a workgroup walks are one stream: copies run two to
+// four steps ahead of the matrix instructions, past a tile's end into the next tile, whose
+// token rows were read a tile earlier, and so do the reads of fragments.  A tile's epilogue,
+// from registers to memory, lies between two steps with the next tile's operands landed or
+// in flight.  Rings in the LDS, and what a step is:
+//   MX4, 256 rows:   256 columns; three slots of A (32 KB), two of B, whose fragments are
+//                    all in registers after a quarter of the step.  Scales go to registers,
+//                    a dword per fragment and step, as the LDS is full.
+//   MX4, 128 rows:   256 columns; three slots of A (16 KB), of B and of scales.
+//   bf16, 256 rows:  64 columns; four slots of A (32 KB) and of weight codes (8 KB).
+//   bf16, 128 rows:  64 columns; five slots of A (16 KB), two of the codes and scales of four
+//                    steps: 128 bytes of a row, a whole line (by 32 bytes each line crosses
+//                    from L2 four times: 0.80 us a step of one 32-row block, 0.43 so).
+// Scales of gathered MX4 activations lie in routed order (that of a gathered row would cost
+// a cache line a step, as much as its codes).
+//
+// In 128-row tiles a wave leaves out 32-row blocks without rows, so ragged experts cost what
+// their rows do: such tiles are dealt tallest first, forward and back (64 experts of 128
+// rows on average, 2048 x 2048, bf16: 95 -> 81 us).
+//
+// Measured on products of even experts: MX4 256 rows 3.3 PFLOP/s, the MFMA's power limit
+// with operands that come from the LDS being 5.9; bf16 256 rows 1.56 PFLOP/s at the margin
+// (a large library product: 1.60), 128 rows 1.36.  Where weights are hardly shared (up to
+// 128 rows an expert) the weights' stream bounds: 5 - 6 TB/s.
 #include <type_traits>
 
 #include "gemm_mx4.hpp"
@@ -758,7 +772,7 @@ struct BigList : TileList {
 __device__ __forceinline__ void build_big_lists(int block, const int32_t* __restrict__ offsets,
                                                 const int32_t* __restrict__ expert_map, int E,
                                                 const BigList& la, const BigList& lb) {
-  __shared__ int s_tmp[4];
+  __shared__ int s_wave[kTableThreads / 64][kClasses];
   __shared__ int s_start[kClasses][kTableThreads];
   __shared__ int s_total[kClasses];
   __shared__ int s_mt[kTableThreads], s_phys[kTableThreads], s_row0[kTableThreads];
@@ -782,11 +796,27 @@ __device__ __forceinline__ void build_big_lists(int block, const int32_t* __rest
       const int cls = L.bm == kClasses * 32 ? kClasses - tall / 32 : 0;
       s_mt[e] = mt;
       s_tall[e] = tall;
+      // sums over the experts before, of all classes at once
+      int sum[kClasses];
+#pragma unroll
+      for (int c = 0; c < kClasses; ++c) sum[c] = cls == c ? mt : 0;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1)
+#pragma unroll
+        for (int c = 0; c < kClasses; ++c) {
+          const int n = __shfl_up(sum[c], off, 64);
+          sum[c] += (e & 63) >= off ? n : 0;
+        }
+      if ((e & 63) == 63)
+#pragma unroll
+        for (int c = 0; c < kClasses; ++c) s_wave[e >> 6][c] = sum[c];
+      __syncthreads();
+#pragma unroll
       for (int c = 0; c < kClasses; ++c) {
-        const int own = mt && cls == c ? mt : 0;
-        const int start = block_excl_scan_256(own, s_tmp);   // (synchronises the block)
-        s_start[c][e] = start;
-        if (e == kTableThreads - 1) s_total[c] = start + own;
+#pragma unroll
+        for (int w = 0; w < kTableThreads / 64; ++w) sum[c] += w < e >> 6 ? s_wave[w][c] : 0;
+        s_start[c][e] = sum[c] - (cls == c ? mt : 0);
+        if (e == kTableThreads - 1) s_total[c] = sum[c];
       }
       __syncthreads();
     }
@@ -842,10 +872,10 @@ __global__ __launch_bounds__(kTableThreads) void mx4_prepare_kernel(
   }
   const long long n = (long long)(gridDim.x - list_blocks) * kTableThreads;
   const int live = offsets[E];                       // rows behind the last expert's: none
-  for (long long r = (long long)(blockIdx.x - list_blocks) * kTableThreads + threadIdx.x;
-       r < g.R && r < live; r += n) {
-    const long long t = g.row_src[r] / g.slots_k;
-    for (int i = 0; i < g.G; ++i) g.dst[i * g.R + r] = g.src[i * g.T + t];
+  for (long long i = (long long)(blockIdx.x - list_blocks) * kTableThreads + threadIdx.x;
+       i < g.R * g.G; i += n) {
+    const long long group = i / g.R, r = i - group * g.R;
+    if (r < live) g.dst[i] = g.src[group * g.T + g.row_src[r] / g.slots_k];
   }
 }
 
@@ -897,7 +927,8 @@ hipError_t launch_mx4_prepare(const int32_t* offsets, const int32_t* expert_map,
   if (routed_scale) {
     g = {reinterpret_cast<const uint64_t*>(x_scale), reinterpret_cast<uint64_t*>(routed_scale),
          row_src, T, R, mx4_groups(K), slots_k};
-    more = (int)(ceil_div(R, kTableThreads) < 4096 ? ceil_div(R, kTableThreads) : 4096);
+    const int64_t n = (R * g.G + kTableThreads - 1) / kTableThreads;
+    more = (int)(n < 4096 ? n : 4096);
   }
   hipLaunchKernelGGL(mx4_prepare_kernel, dim3(blocks + more), dim3(kTableThreads), 0, s, offsets,
                      expert_map, E, la, lb, blocks, g);
