@@ -416,8 +416,10 @@ bool few_rows(int64_t R, int E, int64_t weights, int steps, int products, bool m
 Tiles many_rows(int64_t R, int E, int64_t N, int K, bool mx4) {
   const double live = (double)(R < E ? R : E);
   auto tiles = [&](int bm, int bn) { return ((double)R / bm + live / 2) * ((N + bn - 1) / bn); };
-  // BIG needs k-steps for its pipeline, and offsets within a tile and of scales in 32 bits
-  if (K >= 576 && N <= 1 << 20 && mx4_scale_bytes(R, K) < (size_t)1 << 31) {
+  // BIG needs k-steps for its pipeline, and tiles, offsets within a tile and of scales in 32
+  // bits
+  if (K >= 576 && N <= 1 << 20 && mx4_scale_bytes(R, K) < (size_t)1 << 31 &&
+      tiles(128, 256) < 1 << 29) {
     if (R >= 512 * live && tiles(256, 256) >= (mx4 ? 640 : 900)) return BIG256;
     if (tiles(128, 256) >= 360) return BIG128;
   }

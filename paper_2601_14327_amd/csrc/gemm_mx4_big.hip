@@ -894,14 +894,15 @@ hipError_t launch_big(const Mx4Params& p, int bm, hipStream_t s) {
   return hipGetLastError();
 }
 
-inline int list_max(int64_t R, int E, int bm, int n_tiles) {
-  return (ceil_div(R, bm) + (int)(R < E ? R : E)) * n_tiles;
+inline int64_t list_max(int64_t R, int E, int bm, int n_tiles) {
+  return (ceil_div(R, bm) + (R < E ? R : E)) * n_tiles;
 }
 
 }  // namespace
 
 size_t mx4_big_list_bytes(int64_t R, int E, int bm, int n_cols, bool gate_up) {
-  return table_bytes(list_max(R, E, bm, ceil_div(n_cols, gate_up ? kBigBN / 2 : kBigBN)));
+  const int64_t n = list_max(R, E, bm, ceil_div(n_cols, gate_up ? kBigBN / 2 : kBigBN));
+  return align_up(table_bytes(0) + (size_t)n * sizeof(TileEntry), 256);
 }
 
 hipError_t launch_mx4_prepare(const int32_t* offsets, const int32_t* expert_map, int E, int64_t R,
@@ -910,7 +911,7 @@ hipError_t launch_mx4_prepare(const int32_t* offsets, const int32_t* expert_map,
                               const int32_t* row_src, int slots_k, int64_t T, int K,
                               hipStream_t s) {
   auto list_of = [&](void* at, int rows, int n_tiles) {
-    const int n = list_max(R, E, rows, n_tiles);
+    const int n = (int)list_max(R, E, rows, n_tiles);   // (BIG: under 2^30)
     const TableWs t = carve_table(at, n);
     return BigList{{n_tiles, kFwdTileGroup, n, t.n_entries, t.table}, rows};
   };

@@ -177,3 +177,13 @@ def test_device_tensors_of_other_kinds_are_refused():
         laep.moe_grouped_ffn_fwd_mx4(x, wg, wd, off, act_bits=4, save_act=True, **ok)
     with pytest.raises(laep.LaepError, match="workspace"):
         laep.moe_grouped_ffn_fwd_mx4(x, wg, wd, off, ws=z(16), **ok)
+
+
+def test_workspaces_grow_with_the_rows_past_32_bits():
+    """More tiles than 2^31 (no buffer holds their output): the size does not wrap."""
+    product = [laep.workspace_bytes(laep.LAEP_CALL_MX4_PRODUCT, T, 64, 4, 576, 1 << 20)
+               for T in (1 << 18, 1 << 20, 1 << 22, 1 << 24)]
+    ffn = [laep.workspace_bytes(laep.LAEP_CALL_MX4_FFN, T, 64, 4, 576, 1 << 19)
+           for T in (1 << 18, 1 << 20, 1 << 22, 1 << 24)]
+    for sizes in (product, ffn):
+        assert all(3.9 < b / a < 4.1 for a, b in zip(sizes, sizes[1:]))
