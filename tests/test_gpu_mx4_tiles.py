@@ -117,3 +117,76 @@ def test_rows_left_and_one_expert_with_all(tile, T, E, N, K, act):
     got = host(out)
     assert (np.abs(got - ref)[:live] <= _bound(mag, ref, K, "f32")[:live]).all()
     assert (got[live:] == 7.0).all()
+
+
+def _gpu_ffn(seed, T, k, E, d, f):
+    """Inputs of an FFN made on the device: x, gate/up, down, offsets, row_src."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    row_src, offsets, _ = _routing(np.random.default_rng(seed), T, k, E)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16)
+
+    return (normal(T, d), laep.moe_mx4_quantize(normal(E, 2 * f, d) * d ** -0.5),
+            laep.moe_mx4_quantize(normal(E, d, f) * f ** -0.5), _i32(offsets), _i32(row_src))
+
+
+BIG = [((128, 256), 2100, 4, 20, 1088, 1024), ((256, 256), 16500, 2, 2, 576, 1024)]
+
+
+@pytest.mark.parametrize("act", [4, 16])
+@pytest.mark.parametrize("tile,T,k,E,d,f", BIG)
+def test_graphs_share_a_workspace(tile, T, k, E, d, f, act):
+    """Two captured calls on one workspace, replayed in turn with eager calls of other sizes
+    on the same workspace between: the eager results."""
+    case(f"mx4 ffn in graphs, tile={tile} act={act}")
+    assert laep.laep_mx4_ffn_tile(T * k, E, d, f, act) == tile
+    x, gu, dn, off, src = _gpu_ffn(1, T, k, E, d, f)
+    x2, _, _, off2, src2 = _gpu_ffn(2, T, k, E, d, f)
+    ws = torch.full((laep.workspace_bytes(laep.LAEP_CALL_MX4_FFN, T, k, E, d, f),), 0xFF,
+                    dtype=torch.uint8, device="cuda")
+    kw = dict(k=k, act_bits=act)
+    sets = [(x, off, src), (x2, off2, src2)]
+    eager = [laep.moe_grouped_ffn_fwd_mx4(a, gu, dn, o, row_src=r, **kw)[0] for a, o, r in sets]
+    ys = [torch.empty_like(eager[0]) for _ in sets]
+    graphs = []
+    for (a, o, r), y in zip(sets, ys):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            laep.moe_grouped_ffn_fwd_mx4(a, gu, dn, o, row_src=r, ws=ws, y_perm=y, **kw)
+        graphs.append(graph)
+    one = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+    one[E:] = 1
+    for i in range(6):
+        ys[i % 2].zero_()
+        graphs[i % 2].replay()
+        assert torch.equal(ys[i % 2], eager[i % 2])
+        laep.moe_grouped_ffn_fwd_mx4(x[:1], gu, dn, one, act_bits=act, ws=ws)
+        laep.moe_mx4_grouped_product(x[:700], gu, off.clamp(max=700), ws=ws)
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("act", [4, 16])
+@pytest.mark.parametrize("tile,T,k,E,d,f", BIG)
+def test_calls_at_once(tile, T, k, E, d, f, act):
+    """Calls on two streams, each with a workspace of its own, give what they give alone."""
+    case(f"mx4 ffn on two streams, tile={tile} act={act}")
+    ins = [_gpu_ffn(s, T, k, E, d, f) for s in (3, 4)]
+    kw = dict(k=k, act_bits=act)
+
+    def run(v, **more):
+        return laep.moe_grouped_ffn_fwd_mx4(*v[:4], row_src=v[4], **kw, **more)[0]
+
+    alone = [run(v) for v in ins]
+    ws = [torch.empty(laep.workspace_bytes(laep.LAEP_CALL_MX4_FFN, T, k, E, d, f),
+                      dtype=torch.uint8, device="cuda") for _ in ins]
+    ys = [torch.empty_like(alone[0]) for _ in ins]
+    streams = [torch.cuda.Stream() for _ in ins]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for s, v, w, y in zip(streams, ins, ws, ys):
+            with torch.cuda.stream(s):
+                run(v, ws=w, y_perm=y)
+    torch.cuda.synchronize()
+    for y, want in zip(ys, alone):
+        assert torch.equal(y, want)
