@@ -665,29 +665,32 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
   // A tile's steps in a wave of which the first BLOCKS 32-row blocks have rows.  The last
   // reads are of the next tile, of all blocks.
   auto steps = [&](auto blocks) __attribute__((always_inline)) {
-    if constexpr (MX4) {
-      first_subs(blocks, Early{}, I0{}, 2);          // (nk >= 3)
+    if constexpr (MX4 && LDS_SCALES) {
+      first_subs(blocks, Early{}, I0{}, 0);          // (nk >= 3)
+      for (int kt = 1; kt < nk; ++kt) {
+        if (kt == nk - 2) begin_copies(nxt, more);   // two steps before the tile's end
+        last_sub(blocks, blocks);
+        first_subs(blocks, Later{}, I0{}, 0);
+      }
+      last_sub(blocks, All{});
+    } else if constexpr (MX4) {
+      first_subs(blocks, Early{}, I0{}, 2);
       // step kt, its scales in one set and those of two steps on going there; the copies
       // and scales reach the next tile two steps before its end
       auto step = [&](auto set_tag, int kt) __attribute__((always_inline)) {
         if (kt == nk - 2) {
           begin_copies(nxt, more);
-          if constexpr (!LDS_SCALES) begin_scales(nxt);
+          begin_scales(nxt);
         }
         last_sub(blocks, blocks);
         first_subs(blocks, Later{}, set_tag, kt + 2 < nk ? kt + 2 : kt + 2 - nk);
       };
       int kt = 1;
-      if constexpr (LDS_SCALES) {
-        for (; kt < nk; ++kt) step(I0{}, kt);
-      } else {
-        for (; kt + 1 < nk; kt += 2) {
-          step(I1{}, kt);
-          step(I0{}, kt + 1);
-        }
+      for (; kt + 1 < nk; kt += 2) {
+        step(I1{}, kt);
+        step(I0{}, kt + 1);
       }
-      if (LDS_SCALES) {
-      } else if (kt < nk) {
+      if (kt < nk) {
         step(I1{}, kt);
       } else {                                       // an odd number: the sets change places
 #pragma unroll
@@ -751,7 +754,7 @@ __global__ __launch_bounds__(kBigThreads) void gemm_mx4_big_kernel(Mx4Params p) 
     for (int i = 0; i < TM; ++i) store_block<ACT, EPI, WTM>(p, done, i, wm, wn, lane, acc[i]);
     __builtin_amdgcn_sched_barrier(0);
     if (!go_on) break;
-    finish_rows(nxt, more);                          // (behind the stores: not one is waited for)
+    finish_rows(nxt, more);                          // (loaded ahead of the stores)
   }
   wait_vmcnt<0>();                                   // no copy outlives the workgroup
 }
