@@ -401,27 +401,27 @@ bool few_rows(int64_t R, int E, int64_t weights, int steps, int products, bool m
 // needs some rounds of tiles to even out, and taller tiles of ragged experts waste more.
 // us for one product by 64 x 128 / 128 x 128 / BIG 128 / BIG 256:
 //   experts, N, K         rows   MX4 activations          bf16 activations
-//   64, 2048, 2048        1024   27 / 32 / 30 / 39        39 / 59 / 38 / 82
-//                         4096   38 / 41 / 37 / 51        61 / 77 / 58 / 119
-//                         8192   59 / 46 / 39 / 53        105 / 96 / 76 / 122
-//                        16384   89 / 78 / 59 / 56        176 / 170 / 137 / 140
-//                        32768   189 / 164 / 89 / 89      345 / 303 / 244 / 241
-//   16, 4096, 4096         512   32 / 26 / 33 / 40        53 / 54 / 44 / 77
-//                         2048   42 / 39 / 39 / 59        87 / 88 / 80 / 144
-//                         8192   130 / 101 / 90 / 90      295 / 260 / 244 / 246
-//                        32768   574 / 485 / 297 / 270    1239 / 1128 / 857 / 806
-//   8, 7168, 1024         1024   21 / 18 / 19 / 20        31 / 30 / 30 / 32
-//                         4096   53 / 39 / 33 / 36        84 / 70 / 61 / 74
-//                         8192   95 / 68 / 51 / 47        160 / 130 / 113 / 105
-//   8, 1024, 3584         2048   15 / 16 / 22 / 29        30 / 33 / 44 / 65
-//                         8192   38 / 36 / 37 / 33        79 / 79 / 86 / 71
-//                        16384   69 / 56 / 51 / 57        153 / 134 / 129 / 144
-//   1, 2048, 2048         2048   12 / 12 / 17 / 21        22 / 23 / 31 / 43
-//                         4096   24 / 18 / 20 / 24        47 / 36 / 37 / 46
-//                        16384   81 / 70 / 47 / 46        174 / 171 / 113 / 105
-//   32, 1024, 1024        4096   14 / 11 / 14 / 17        20 / 18 / 22 / 28
-//                        16384   32 / 26 / 25 / 27        49 / 44 / 46 / 51
-// Over 63 such cases the rule takes on average 0.6 % (MX4) and 1.4 % (bf16) longer than the
+//   64, 2048, 2048        1024   26 / 31 / 29 / 39        39 / 60 / 37 / 83
+//                         4096   32 / 41 / 36 / 51        58 / 77 / 58 / 118
+//                         8192   50 / 46 / 38 / 52        96 / 95 / 75 / 119
+//                        16384   77 / 78 / 59 / 54        170 / 172 / 141 / 138
+//                        32768   172 / 165 / 90 / 88      326 / 308 / 244 / 242
+//   16, 4096, 4096         512   30 / 26 / 30 / 38        46 / 54 / 44 / 76
+//                         2048   37 / 39 / 36 / 57        82 / 88 / 79 / 144
+//                         8192   118 / 101 / 86 / 86      285 / 264 / 241 / 242
+//                        32768   537 / 484 / 296 / 270    1203 / 1118 / 861 / 808
+//   8, 7168, 1024         1024   17 / 18 / 18 / 19        27 / 29 / 30 / 30
+//                         4096   42 / 39 / 32 / 35        72 / 70 / 61 / 72
+//                         8192   78 / 70 / 52 / 46        146 / 134 / 112 / 103
+//   8, 1024, 3584         2048   15 / 16 / 20 / 27        30 / 33 / 44 / 64
+//                         8192   32 / 35 / 34 / 30        72 / 78 / 84 / 69
+//                        16384   61 / 55 / 49 / 54        135 / 133 / 127 / 141
+//   1, 2048, 2048         2048   12 / 12 / 16 / 20        23 / 23 / 30 / 42
+//                         4096   23 / 17 / 18 / 23        45 / 35 / 35 / 45
+//                        16384   71 / 70 / 45 / 44        177 / 172 / 110 / 103
+//   32, 1024, 1024        4096   11 / 10 / 13 / 16        17 / 18 / 21 / 27
+//                        16384   27 / 26 / 24 / 26        45 / 43 / 45 / 50
+// Over 63 such cases the rule takes on average 0.4 % (MX4) and 1.1 % (bf16) longer than the
 // best tiles.
 Tiles many_rows(int64_t R, int E, int64_t N, int K, bool mx4) {
   const double live = (double)(R < E ? R : E);
@@ -431,9 +431,13 @@ Tiles many_rows(int64_t R, int E, int64_t N, int K, bool mx4) {
   if (K >= 576 && N <= 1 << 20 && mx4_scale_bytes(R, K) < (size_t)1 << 31 &&
       tiles(128, 256) < 1 << 29) {
     if (R >= 512 * live && tiles(256, 256) >= (mx4 ? 640 : 900)) return BIG256;
-    if (tiles(128, 256) >= 360) return BIG128;
+    // (64-row tiles are as good for up to 64 rows an expert)
+    if (R >= 96 * live && tiles(128, 256) >= 360) return BIG128;
   }
-  return R >= (mx4 ? 32 : 128) * live && tiles(64, 128) >= (mx4 ? 500 : 540) ? MID128 : MID64;
+  // 768 tiles of 64 rows run at once, 512 of 128
+  const double n = tiles(64, 128);
+  const bool tall = n >= 2000 || (n >= 500 && (R >= 2048 * live || (mx4 && n <= 800)));
+  return R >= 32 * live && tall ? MID128 : MID64;
 }
 Tiles product_tiles(int64_t R, int E, int N, int K, bool mx4) {
   return few_rows(R, E, (int64_t)N * K, mx4_groups(K), 1, mx4) ? FEW : many_rows(R, E, N, K, mx4);

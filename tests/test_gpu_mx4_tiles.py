@@ -64,9 +64,9 @@ def test_product(tile, T, k, E, dead, N, K, act, dtype):
 
 FFNS = [   # the two products' tiles; T, k, E, dead, d, f
     ((64, 128), (128, 256), 1000, 2, 8, 1, 7168, 640),
-    ((128, 128), (64, 128), 1500, 2, 16, 3, 320, 704),
+    ((128, 128), (64, 128), 3200, 2, 2, 0, 320, 704),
     ((128, 256), (128, 256), 1000, 8, 20, 0, 1088, 1024),
-    ((128, 256), (128, 128), 8800, 1, 20, 2, 576, 1216),
+    ((128, 256), (128, 128), 8800, 1, 4, 1, 576, 1216),
     ((256, 256), (128, 256), 16500, 2, 2, 0, 576, 1024),
     ((256, 256), (128, 128), 9000, 1, 2, 0, 640, 3584)]
 
