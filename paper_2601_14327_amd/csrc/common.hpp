@@ -19,6 +19,15 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
 constexpr int kWave = 64;
 
+// A grid of any number of workgroups, and a workgroup's index in it (the last ones may lie
+// past the number).  Two dimensions: one holds less than 2^32 threads, and a launch past
+// that is cut off without an error.  (2^20 in a row: the index mod 8 stays the XCD.)
+inline dim3 grid_of(int64_t blocks) {
+  if (blocks <= 1 << 20) return dim3((unsigned)blocks);
+  return dim3(1 << 20, (unsigned)((blocks + (1 << 20) - 1) >> 20));
+}
+__device__ __forceinline__ unsigned block_index() { return blockIdx.y << 20 | blockIdx.x; }
+
 // ---------------------------------------------------------------------------
 // bf16 <-> fp32.  bf16 keeps the sign, the 8 exponent bits and the top 7
 // fraction bits of binary32.  Narrowing uses gfx950's v_cvt_pk_bf16_f32

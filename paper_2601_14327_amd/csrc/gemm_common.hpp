@@ -118,6 +118,7 @@ __device__ __forceinline__ uint32_t div_slots(uint32_t n, uint32_t k, uint32_t m
 
 inline int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 inline int round8(int v) { return (v + 7) & ~7; }
+inline dim3 tile_grid(int64_t tiles) { return grid_of((tiles + 7) & ~(int64_t)7); }
 
 }  // namespace
 }  // namespace laep

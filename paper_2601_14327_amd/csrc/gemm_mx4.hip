@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kMx4GemmThreads) void gemm_mx4_kernel(Mx4Params p) 
   const int wave = tid >> 6, lane = tid & 63, half = lane >> 5;
   const int wave_s = __builtin_amdgcn_readfirstlane(wave);
   FoundTile te;
-  if (!find_tile(blockIdx.x, p.offsets, p.expert_map, p.E, BM, p.n_tiles_n, smem, te)) return;
+  if (!find_tile(block_index(), p.offsets, p.expert_map, p.E, BM, p.n_tiles_n, smem, te)) return;
   const int nt = te.nt;
   const int wm = wave / 2, wn = wave % 2;
 
@@ -350,7 +350,7 @@ template <int BM, int NST, int ACT, int EPI>
 hipError_t launch_tiles(const Mx4Params& p, int64_t R, hipStream_t s) {
   const int64_t tiles = most_tiles(p, BM, R);
   if (tiles <= 0) return hipSuccess;
-  hipLaunchKernelGGL((gemm_mx4_kernel<BM, NST, ACT, EPI>), dim3(round8((int)tiles)),
+  hipLaunchKernelGGL((gemm_mx4_kernel<BM, NST, ACT, EPI>), tile_grid(tiles),
                      dim3(kMx4GemmThreads), 0, s, p);
   return hipGetLastError();
 }

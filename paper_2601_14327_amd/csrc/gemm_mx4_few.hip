@@ -122,7 +122,8 @@ __global__ __launch_bounds__(64 * kFewSplit, 4) void gemm_mx4_few_kernel(Mx4Para
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   FewTile te;
-  if (!few_tile(blockIdx.x & 7, blockIdx.x >> 3, p.offsets, p.expert_map, p.E, p.n_tiles_n, lane,
+  const unsigned block = block_index();
+  if (!few_tile(block & 7, block >> 3, p.offsets, p.expert_map, p.E, p.n_tiles_n, lane,
                 te))
     return;
 
@@ -308,7 +309,7 @@ template <int AKIND, int EPI>
 hipError_t launch_few(const Mx4Params& p, int64_t R, hipStream_t s) {
   // sum of ceil(rows / kFewBM) over the experts with rows
   const int64_t tiles = (R / kFewBM + (R < p.E ? R : p.E)) * p.n_tiles_n;
-  hipLaunchKernelGGL((gemm_mx4_few_kernel<AKIND, EPI>), dim3(round8((int)tiles)),
+  hipLaunchKernelGGL((gemm_mx4_few_kernel<AKIND, EPI>), tile_grid(tiles),
                      dim3(64 * kFewSplit), 0, s, p);
   return hipGetLastError();
 }
