@@ -25,7 +25,8 @@ __host__ __device__ inline int tokens_per_block(int vec_per_row) {
 __global__ __launch_bounds__(kRowThreads) void permute_kernel(
     const u32x4_t* __restrict__ x, const int32_t* __restrict__ dest_row, int n_tok, int k,
     int vec_per_row, int tpb, u32x4_t* __restrict__ x_perm) {
-  const int t_lo = blockIdx.x * tpb;
+  if ((long long)block_index() * tpb >= n_tok) return;
+  const int t_lo = block_index() * tpb;
   const int n_vec = tpb * vec_per_row;
   for (int i = threadIdx.x; i < n_vec; i += kRowThreads) {
     const int t = t_lo + i / vec_per_row;
@@ -45,7 +46,7 @@ __global__ __launch_bounds__(kRowThreads) void permute_kernel(
 __global__ __launch_bounds__(kRowThreads) void gather_rows_kernel(
     const u32x4_t* __restrict__ x, const int32_t* __restrict__ row_src, int k, int64_t R,
     int vec_per_row, u32x4_t* __restrict__ x_perm) {
-  const long long i = (long long)blockIdx.x * kRowThreads + threadIdx.x;
+  const long long i = (long long)block_index() * kRowThreads + threadIdx.x;
   if (i >= R * vec_per_row) return;
   const long long r = i / vec_per_row;
   const int v = (int)(i % vec_per_row);
@@ -101,7 +102,8 @@ __global__ __launch_bounds__(kRowThreads) void combine_kernel(
     int n_tok, int k, int d, int tpb, T* __restrict__ out) {
   constexpr int UNR = sizeof(T) == 2 ? 2 : 1;
   const int vec_per_row = d / 8;
-  const int t_lo = blockIdx.x * tpb;
+  if ((long long)block_index() * tpb >= n_tok) return;
+  const int t_lo = block_index() * tpb;
   const int n_vec = tpb * vec_per_row;
   for (int i0 = threadIdx.x; i0 < n_vec; i0 += UNR * kRowThreads) {
     int t[UNR], v[UNR];
@@ -159,7 +161,8 @@ __global__ __launch_bounds__(kRowThreads) void combine_bwd_kernel(
     const int32_t* __restrict__ dest_row, int n_tok, int k, int d, T* __restrict__ dy,
     float* __restrict__ dgate) {
   __shared__ float s_red[kRowThreads / 64];
-  const int t = blockIdx.x;
+  if (block_index() >= (unsigned)n_tok) return;
+  const int t = block_index();
   const int vec_per_row = d / 8;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const T* drow = dout + (size_t)t * d;
@@ -202,7 +205,7 @@ hipError_t launch_permute(const void* x, int elem_bytes, const int32_t* dest_row
   if (T == 0) return hipSuccess;
   const int vec_per_row = d * elem_bytes / 16;
   const int tpb = tokens_per_block(vec_per_row);
-  hipLaunchKernelGGL(permute_kernel, dim3((T + tpb - 1) / tpb), dim3(kRowThreads), 0, s,
+  hipLaunchKernelGGL(permute_kernel, grid_of(((int64_t)T + tpb - 1) / tpb), dim3(kRowThreads), 0, s,
                      static_cast<const u32x4_t*>(x), dest_row, T, k, vec_per_row, tpb,
                      static_cast<u32x4_t*>(x_perm));
   return hipGetLastError();
@@ -213,7 +216,7 @@ hipError_t launch_gather_rows(const void* x, const int32_t* row_src, int k, int6
   if (R == 0) return hipSuccess;
   const int vec_per_row = d * elem_bytes / 16;
   const long long n = R * (long long)vec_per_row;
-  hipLaunchKernelGGL(gather_rows_kernel, dim3((unsigned)((n + kRowThreads - 1) / kRowThreads)),
+  hipLaunchKernelGGL(gather_rows_kernel, grid_of((n + kRowThreads - 1) / kRowThreads),
                      dim3(kRowThreads), 0, s, static_cast<const u32x4_t*>(x), row_src, k, R,
                      vec_per_row, static_cast<u32x4_t*>(x_perm));
   return hipGetLastError();
@@ -223,7 +226,7 @@ hipError_t launch_combine(const void* y, const float* gate, const int32_t* dest_
                           int d, int dtype, void* out, hipStream_t s) {
   if (T == 0) return hipSuccess;
   const int tpb = tokens_per_block(d / 8);
-  dim3 grid((T + tpb - 1) / tpb), block(kRowThreads);
+  const dim3 grid = grid_of(((int64_t)T + tpb - 1) / tpb), block(kRowThreads);
   if (dtype == kDtypeBf16) {
     if (gate)
       hipLaunchKernelGGL((combine_kernel<bf16_t, true>), grid, block, 0, s,
@@ -251,11 +254,11 @@ hipError_t launch_combine_bwd(const void* dout, const void* y, const float* gate
                               float* dgate, hipStream_t s) {
   if (T == 0) return hipSuccess;
   if (dtype == kDtypeBf16)
-    hipLaunchKernelGGL((combine_bwd_kernel<bf16_t>), dim3(T), dim3(kRowThreads), 0, s,
+    hipLaunchKernelGGL((combine_bwd_kernel<bf16_t>), grid_of(T), dim3(kRowThreads), 0, s,
                        static_cast<const bf16_t*>(dout), static_cast<const bf16_t*>(y), gate,
                        dest_row, T, k, d, static_cast<bf16_t*>(dy), dgate);
   else
-    hipLaunchKernelGGL((combine_bwd_kernel<float>), dim3(T), dim3(kRowThreads), 0, s,
+    hipLaunchKernelGGL((combine_bwd_kernel<float>), grid_of(T), dim3(kRowThreads), 0, s,
                        static_cast<const float*>(dout), static_cast<const float*>(y), gate,
                        dest_row, T, k, d, static_cast<float*>(dy), dgate);
   return hipGetLastError();

@@ -1,0 +1,50 @@
+"""Calls of more workgroups than one grid dimension holds (2^32 threads): every output is
+written."""
+import pytest
+import torch
+
+import paper_2601_14327_amd as laep
+from _gpu import case
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+def _last_rows(T, d):
+    """Zeros, 1 to 3 in the last three rows."""
+    x = torch.zeros((T, d), dtype=BF16, device="cuda")
+    x[-3:] = torch.arange(1.0, 4.0, device="cuda")[:, None].to(BF16)
+    return x
+
+
+def _nan(*shape, dtype=BF16):
+    return torch.full(shape, float("nan"), dtype=dtype, device="cuda")
+
+
+def test_rows_of_2_to_the_28_tokens():
+    """Dispatch and both sums over a token's rows, one row each: copies."""
+    T, d = (1 << 28) + 70, 8
+    case(f"permute, combine, permute backward T={T} d={d}")
+    x, dest = _last_rows(T, d), torch.arange(T, dtype=torch.int32, device="cuda")
+    out = _nan(T, d)
+    laep.moe_permute(x, dest, 1, out=out)
+    assert torch.equal(out, x)
+    out.fill_(float("nan"))
+    laep.moe_permute_bwd(x, dest, T, 1, out=out)
+    assert torch.equal(out, x)
+    out.fill_(float("nan"))
+    laep.moe_combine(x, torch.ones((T, 1), device="cuda"), dest, out=out)
+    assert torch.equal(out, x)
+    del x, dest, out
+    torch.cuda.empty_cache()
+
+
+def test_combine_backward_of_2_to_the_24_tokens():
+    T, d = (1 << 24) + 70, 8
+    case(f"combine backward T={T} d={d}")
+    x, dest = _last_rows(T, d), torch.arange(T, dtype=torch.int32, device="cuda")
+    gate, dy, dgate = torch.full((T, 1), 2.0, device="cuda"), _nan(T, d), \
+        _nan(T, 1, dtype=torch.float32)
+    laep.moe_combine_bwd(x, x, gate, dest, dy_perm=dy, dgate=dgate)
+    assert torch.equal(dy, 2 * x)
+    assert dgate[-3:, 0].tolist() == [8.0, 32.0, 72.0] and not dgate[:-3].any()
