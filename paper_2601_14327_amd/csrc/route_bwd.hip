@@ -199,8 +199,8 @@ __global__ __launch_bounds__(256) void route_bwd_dx_kernel(
     const T* __restrict__ w_router, const int32_t* __restrict__ ids,
     const float* __restrict__ dl, int n_tok, int slots, int d, int accumulate,
     T* __restrict__ dx) {
-  const int t = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (int)(threadIdx.x >> 6));
-  if (t >= n_tok) return;
+  const unsigned t = __builtin_amdgcn_readfirstlane(block_index() * 4 + (threadIdx.x >> 6));
+  if (t >= (unsigned)n_tok) return;
   const int lane = threadIdx.x & 63;
   const int vec_per_row = d / 8;
   const size_t o = (size_t)t * slots;
@@ -720,7 +720,7 @@ hipError_t launch_route_bwd_t(const float* dgate, const int32_t* idx, const floa
       if (err != hipSuccess) return err;
     }
     if (dx && dx_by_rows(T_, E))
-      hipLaunchKernelGGL(route_bwd_dx_kernel<T>, dim3((unsigned)((T_ + 3) / 4)), dim3(256), 0, s,
+      hipLaunchKernelGGL(route_bwd_dx_kernel<T>, grid_of(((int64_t)T_ + 3) / 4), dim3(256), 0, s,
                          w_router, static_cast<const int32_t*>(nullptr), dl_dense, T_, E, d,
                          accumulate_dx, dx);
     else if (dx)
@@ -742,7 +742,7 @@ hipError_t launch_route_bwd_t(const float* dgate, const int32_t* idx, const floa
                        gate, T_, E, k, dl, dense ? dl_dense : nullptr, dlogits);
   }
   if (dx)
-    hipLaunchKernelGGL(route_bwd_dx_kernel<T>, dim3((unsigned)((T_ + 3) / 4)), dim3(256), 0, s,
+    hipLaunchKernelGGL(route_bwd_dx_kernel<T>, grid_of(((int64_t)T_ + 3) / 4), dim3(256), 0, s,
                        w_router, idx, dl, T_, k, d, accumulate_dx, dx);
   if (dense) {
     launch_dense_dw<T, true>(dl_dense, x, T_, E, d, base, dw_router, dbias, idx, k, s);

@@ -48,3 +48,22 @@ def test_combine_backward_of_2_to_the_24_tokens():
     laep.moe_combine_bwd(x, x, gate, dest, dy_perm=dy, dgate=dgate)
     assert torch.equal(dy, 2 * x)
     assert dgate[-3:, 0].tolist() == [8.0, 32.0, 72.0] and not dgate[:-3].any()
+
+
+@pytest.mark.parametrize("renorm", [True, False])
+def test_router_backward_data_of_2_to_the_26_tokens(renorm):
+    T, E, k, d = (1 << 26) + 70, 2, 1, 8
+    case(f"router backward, data T={T} E={E} d={d} renorm={renorm}")
+    idx = torch.zeros((T, k), dtype=torch.int32, device="cuda")
+    gate, dg = torch.ones((T, k), device="cuda"), torch.zeros((T, k), device="cuda")
+    gate[-3:], dg[-3:] = 0.5, 4.0
+    x, wr = torch.zeros((T, d), dtype=BF16, device="cuda"), _nan(E, d)
+    wr[0], wr[1] = 1.0, 3.0
+    dx = _nan(T, d)
+    logits = None if renorm else torch.zeros((T, E), device="cuda")
+    off = torch.tensor([0, T, T], dtype=torch.int32, device="cuda")
+    src = torch.arange(T, dtype=torch.int32, device="cuda")
+    laep.moe_route_bwd(dg, idx, gate, x, wr, renorm=renorm, logits=logits, offsets=off, row_src=src,
+                       dx=dx, weights=False)
+    # s = g dg = 2; renorm: dl = g (dg - s) = 1 at expert 0; full: p (q - s) = 1 and -1
+    assert (dx[-3:] == (1.0 if renorm else -2.0)).all() and not dx[:-3].any()
