@@ -191,7 +191,9 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(
   const int tid = threadIdx.x;
   const int wave = tid >> 6;
   const int lane = tid & 63;
-  const int t0 = blockIdx.x * kRouteTokens;
+  const unsigned block = block_index();
+  if (block >= (unsigned)((n_tok - 1) / kRouteTokens + 1)) return;
+  const int t0 = block * kRouteTokens;
 
   // expert e = tid (EP <= 256 < the thread count): its bias and alive flag are
   // loaded now and stored to LDS after the GEMM, so the operand loads are
@@ -256,7 +258,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(
     char* const s_w = s_stage + NSX * St::XS;
     // Workgroups on one XCD (block i runs on XCD i % 8) start at different
     // chunks, so they do not all request the same W_r lines at once.
-    const int rot = (int)((blockIdx.x >> 3) % n_chunks);
+    const int rot = (int)((block >> 3) % n_chunks);
     auto rotated = [&](int c) {
       const int cl = c < n_chunks ? c : n_chunks - 1;
       return cl + rot < n_chunks ? cl + rot : cl + rot - n_chunks;
@@ -572,9 +574,9 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(
     // mask word of (wave tile blockIdx/2, expert e): tokens 0-31 of the tile
     // in the low word, 32-63 in the high word; a last even workgroup also
     // clears the high word (no tokens there)
-    const size_t wt = blockIdx.x >> 1;
-    const int half = blockIdx.x & 1;
-    const bool clear_hi = half == 0 && blockIdx.x == gridDim.x - 1;
+    const size_t wt = block >> 1;
+    const int half = block & 1;
+    const bool clear_hi = half == 0 && n_tok - t0 <= kRouteTokens;
     for (int e = tid; e < E; e += kRouteThreads) {
       masks32[2 * (wt * E + e) + half] = s_mask[e];
       if (clear_hi) masks32[2 * (wt * E + e) + 1] = 0u;
@@ -607,7 +609,7 @@ hipError_t launch_route_t(const void* x, const void* w, const float* bias, const
                           int T_, int d, int E, int k, int renorm, float* logits, int32_t* idx,
                           float* gate, uint32_t* masks32, hipStream_t s) {
   const int nb = (E + 31) / 32;
-  const dim3 grid((T_ + kRouteTokens - 1) / kRouteTokens);
+  const dim3 grid = grid_of(((int64_t)T_ + kRouteTokens - 1) / kRouteTokens);
   // bf16 with up to 128 experts: LDS-staged chunks of 256 (NB <= 2) or 128 columns
   int kc = 0;
   if (sizeof(T) == 2 && nb <= 4) {

@@ -67,3 +67,22 @@ def test_router_backward_data_of_2_to_the_26_tokens(renorm):
                        dx=dx, weights=False)
     # s = g dg = 2; renorm: dl = g (dg - s) = 1 at expert 0; full: p (q - s) = 1 and -1
     assert (dx[-3:] == (1.0 if renorm else -2.0)).all() and not dx[:-3].any()
+
+
+def test_routing_of_2_to_the_28_tokens():
+    T, E, k, d = (1 << 28) + 70, 2, 1, 8
+    case(f"routing and counts T={T} E={E} d={d}")
+    x, wr = _last_rows(T, d), torch.zeros((E, d), dtype=BF16, device="cuda")
+    wr[1] = 1.0
+    idx = torch.full((T, k), -7, dtype=torch.int32, device="cuda")
+    gate = _nan(T, k, dtype=torch.float32)
+    src = torch.full((T,), -7, dtype=torch.int32, device="cuda")
+    dest = torch.full((T,), -7, dtype=torch.int32, device="cuda")
+    _, _, counts, offsets, _, _, _ = laep.moe_route_count(
+        x, wr, k, want_row_src=True, topk_idx=idx, topk_gate=gate, dest_row=dest, row_src=src)
+    assert idx[-3:, 0].tolist() == [1, 1, 1] and not idx[:-3].any() and (gate == 1.0).all()
+    assert counts.tolist() == [T - 3, 3] and offsets.tolist() == [0, T - 3, T]
+    rows = torch.arange(T, dtype=torch.int32, device="cuda")
+    assert torch.equal(src, rows) and torch.equal(dest, rows)
+    del x, idx, gate, src, dest, rows
+    torch.cuda.empty_cache()
