@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kSmallThreads) void gemm_small_kernel(SmallParams p
   const int tid = threadIdx.x;
   const int wave = tid >> 6, lane = tid & 63;
   FoundTile te;
-  if (!find_tile(blockIdx.x, p.offsets, p.expert_map, p.E, BM, p.n_tiles_n, smem, te)) return;
+  if (!find_tile(block_index(), p.offsets, p.expert_map, p.E, BM, p.n_tiles_n, smem, te)) return;
   const int nt = te.nt;
 
   const int wave_s = __builtin_amdgcn_readfirstlane(wave);
@@ -266,7 +266,7 @@ hipError_t launch_small(const SmallParams& p, int64_t R, hipStream_t s) {
   // sum of ceil(rows / BM) over the experts with rows
   const int64_t tiles = (R / BM + (R < p.E ? R : p.E)) * p.n_tiles_n;
   if (tiles <= 0) return hipSuccess;
-  hipLaunchKernelGGL((gemm_small_kernel<BM, NST, EPI, GATHER>), dim3(round8((int)tiles)),
+  hipLaunchKernelGGL((gemm_small_kernel<BM, NST, EPI, GATHER>), tile_grid(tiles),
                      dim3(kSmallThreads), 0, s, p);
   return hipGetLastError();
 }

@@ -86,3 +86,32 @@ def test_routing_of_2_to_the_28_tokens():
     assert torch.equal(src, rows) and torch.equal(dest, rows)
     del x, idx, gate, src, dest, rows
     torch.cuda.empty_cache()
+
+
+def test_ffn_of_2_to_the_24_tiles():
+    """One row an expert, all 256 of one matrix of 2^22 hidden columns."""
+    R, E, d, f = 256, 256, 64, 1 << 22
+    case(f"ffn R={R} E={E} d={d} f={f}")
+    assert laep.laep_ffn_fwd_row_tile(R, E, d, f) == 32
+    assert (R // 32 + E) * (f // 64) > 1 << 24
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((R, d), generator=g, device="cuda").to(BF16)
+    gu = torch.randn((1, 2 * f, d), generator=g, device="cuda", dtype=BF16) * 0.125
+    dn = torch.zeros((1, d, f), device="cuda", dtype=BF16)
+    dn[0, :, -64:] = torch.eye(64, device="cuda").to(BF16)      # y: the last columns of H
+    off = torch.arange(E + 1, dtype=torch.int32, device="cuda")
+    emap = torch.zeros(E, dtype=torch.int32, device="cuda")
+    act = _nan(R, 2 * f)
+    ws = torch.full((laep.workspace_bytes(laep.LAEP_CALL_FFN_FWD, R, 1, E, d, f),), 0xFF,
+                    dtype=torch.uint8, device="cuda")
+    y, _ = laep.moe_grouped_ffn_fwd(x, gu, dn, off, expert_map=emap, act_save=act, ws=ws)
+    for rows in act.split(16):
+        assert torch.isfinite(rows).all()
+    xv, gv, uv = (v.double().cpu() for v in (x, gu[0, f - 64:f], gu[0, 2 * f - 64:]))
+    a, u = xv @ gv.T, xv @ uv.T
+    h = a * torch.sigmoid(a) * u
+    # A rounded, then H and y: half a step each of values of their own size
+    assert ((act[:, f - 64:f].double().cpu() - a).abs() <= 2.0 ** -8 * a.abs() + 1e-4).all()
+    assert ((y.double().cpu() - h).abs() <= 3 * 2.0 ** -8 * h.abs() + 1e-4).all()
+    del act, gu, dn, ws
+    torch.cuda.empty_cache()
