@@ -69,7 +69,7 @@ int laep_ffn_fwd_row_tile(int64_t R, int E, int d_model, int d_ff);
  * not wanted) its columns (64, 128 or 256), for R = T * k rows (T without
  * row_src) and activations of act_bits (4: MX4, 16: bf16); of the FFN's gate/up
  * product, or (down) of its second.  Host code only; 0 for sizes that those calls
- * refuse.
+ * refuse (their limit on x, which T sets, apart).
  */
 int laep_mx4_product_tile(int64_t R, int E, int N, int K, int act_bits, int* cols);
 int laep_mx4_ffn_tile(int64_t R, int E, int d_model, int d_ff, int act_bits, int down, int* cols);

@@ -938,6 +938,14 @@ int check_mx4_act(const char* name, int64_t rows, int64_t K, bool mx4) {
 
 size_t mx4_scale_bytes(int64_t R, int64_t C) { return (size_t)((C + 255) / 256) * R * 8; }
 
+// the scales of H in MX4, addressed over all rows with 32-bit byte offsets
+int check_mx4_h(const char* name, int64_t R, int64_t d_ff, int act_bits) {
+  REQUIRE(act_bits == 16 || mx4_scale_bytes(R, d_ff) < (size_t)kMaxBufferBytes,
+          LAEP_ERR_UNSUPPORTED, "%s: R=%lld rows of d_ff=%lld are too many in one call", name,
+          (long long)R, (long long)d_ff);
+  return LAEP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1029,10 +1037,7 @@ int moe_grouped_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int k,
   if ((rc = check_mx4_shape(name, 2 * (int64_t)d_ff, d_model))) return rc;
   if ((rc = check_mx4_shape(name, d_model, d_ff))) return rc;
   if ((rc = check_mx4_act(name, T, d_model, false))) return rc;
-  // H's scales are addressed over all rows
-  REQUIRE(act_bits == 16 || mx4_scale_bytes(R, d_ff) < (size_t)kMaxBufferBytes,
-          LAEP_ERR_UNSUPPORTED, "%s: R=%lld rows of d_ff=%d are too many in one call", name,
-          (long long)R, d_ff);
+  if ((rc = check_mx4_h(name, R, d_ff, act_bits))) return rc;
   REQUIRE(offsets, LAEP_ERR_INVALID_ARG, "%s: offsets must be non-null", name);
   if (R == 0) return ok();
   REQUIRE(x && w_gate_up && w_gate_up_scale && w_down && w_down_scale && y_perm && ws,
@@ -1110,7 +1115,8 @@ int laep_mx4_ffn_tile(int64_t R, int E, int d_model, int d_ff, int act_bits, int
   const char* const name = "laep_mx4_ffn_tile";
   if ((act_bits != 4 && act_bits != 16) || R > 0x7FFFFFFFll ||
       check_mx4_rows(name, nullptr, (int)R, 1, E, R) ||
-      check_mx4_shape(name, 2 * (int64_t)d_ff, d_model) || check_mx4_shape(name, d_model, d_ff))
+      check_mx4_shape(name, 2 * (int64_t)d_ff, d_model) || check_mx4_shape(name, d_model, d_ff) ||
+      check_mx4_h(name, R, d_ff, act_bits))
     return 0;
   return laep::mx4_ffn_tile(R, E, d_model, d_ff, act_bits == 4, down != 0, cols);
 }
