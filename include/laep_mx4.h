@@ -70,7 +70,8 @@ int moe_mx4_dequantize(const uint8_t* codes, const uint8_t* scale, int dtype,
  *            expert's range, are left as they were in out
  *   out      device [R, N] out_dtype
  *   K % 64 == 0, N % 64 == 0; x, one slot of w, and each scale array of x under
- *   2 GiB; out must not overlap the inputs.
+ *   2 GiB; out and ws must not overlap the inputs or each other (of w, a call with an
+ *   expert_map checks the first slot only).
  *   Workspace: moe_workspace_bytes(LAEP_CALL_MX4_PRODUCT, T, k, E, K, N).
  */
 int moe_mx4_grouped_product(const void* x, const uint8_t* x_scale,
@@ -96,7 +97,8 @@ int moe_mx4_grouped_product(const void* x, const uint8_t* x_scale,
  *            quantisation-aware training are moe_grouped_ffn_bwd_gather's at
  *            this act_save and at the weights' values (moe_mx4_dequantize).
  *   d_model % 64 == 0, d_ff % 64 == 0; rows left as they were, and limits, as in
- *   moe_mx4_grouped_product.  y_perm and act_save must not overlap the inputs.
+ *   moe_mx4_grouped_product.  y_perm, act_save and ws must not overlap the inputs or
+ *   each other, likewise.
  *   Workspace: moe_workspace_bytes(LAEP_CALL_MX4_FFN, T, k, E, d_model, d_ff)
  *   (either act_bits; without row_src T and k as given).
  */

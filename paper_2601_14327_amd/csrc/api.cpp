@@ -938,6 +938,25 @@ int check_mx4_act(const char* name, int64_t rows, int64_t K, bool mx4) {
 
 size_t mx4_scale_bytes(int64_t R, int64_t C) { return (size_t)((C + 255) / 256) * R * 8; }
 
+// Outputs and the workspace share no bytes with the inputs, nor with each other.  Of the
+// weights: the E slots that a call without a map reads, or the first (the map is on the device).
+struct Bytes {
+  const void* p;
+  size_t n;
+};
+template <size_t NOUT, size_t NIN>
+int check_mx4_overlap(const char* name, const char* outs, const Bytes (&out)[NOUT],
+                      const Bytes (&in)[NIN]) {
+  bool shared = false;
+  for (size_t i = 0; i < NOUT; ++i) {
+    for (const Bytes& b : in) shared |= overlap(out[i].p, out[i].n, b.p, b.n);
+    for (size_t j = 0; j < i; ++j) shared |= overlap(out[i].p, out[i].n, out[j].p, out[j].n);
+  }
+  REQUIRE(!shared, LAEP_ERR_INVALID_ARG, "%s: %s must not overlap the inputs or each other", name,
+          outs);
+  return LAEP_OK;
+}
+
 // the scales of H in MX4, addressed over all rows with 32-bit byte offsets
 int check_mx4_h(const char* name, int64_t R, int64_t d_ff, int act_bits) {
   REQUIRE(act_bits == 16 || mx4_scale_bytes(R, d_ff) < (size_t)kMaxBufferBytes,
@@ -1007,14 +1026,17 @@ int moe_mx4_grouped_product(const void* x, const uint8_t* x_scale, const int32_t
           LAEP_ERR_INVALID_ARG, "%s: buffers must be 16-byte aligned", name);
   REQUIRE(ws_bytes >= need, LAEP_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", name, ws_bytes,
           need);
-  const size_t out_bytes = (size_t)R * N * elem_bytes(out_dtype);
-  const size_t x_bytes = x_scale ? (size_t)T * K / 2 : (size_t)T * K * 2;
-  REQUIRE(!overlap(out, out_bytes, x, x_bytes) &&
-              !overlap(out, out_bytes, x_scale, mx4_scale_bytes(T, K)) &&
-              !overlap(out, out_bytes, w, (size_t)N * K / 2) &&
-              !overlap(out, out_bytes, w_scale, mx4_scale_bytes(N, K)) &&
-              !overlap(out, out_bytes, ws, need),
-          LAEP_ERR_INVALID_ARG, "%s: out must not overlap the inputs or ws", name);
+  const size_t slots = expert_map ? 1 : E;
+  rc = check_mx4_overlap(
+      name, "out and ws", {{out, (size_t)R * N * elem_bytes(out_dtype)}, {ws, need}},
+      {{x, x_scale ? (size_t)T * K / 2 : (size_t)T * K * 2},
+       {x_scale, mx4_scale_bytes(T, K)},
+       {row_src, (size_t)R * 4},
+       {w, slots * N * K / 2},
+       {w_scale, slots * mx4_scale_bytes(N, K)},
+       {offsets, (size_t)(E + 1) * 4},
+       {expert_map, (size_t)E * 4}});
+  if (rc) return rc;
   return hip_status(laep::launch_mx4_product(x, x_scale, row_src, T, k, w, w_scale, offsets,
                                              expert_map, out_dtype, E, N, K, R, out, ws,
                                              as_stream(stream)),
@@ -1050,21 +1072,19 @@ int moe_grouped_ffn_fwd_mx4(const void* x, const int32_t* row_src, int T, int k,
   const size_t need = laep::ffn_fwd_mx4_ws_bytes(T, row_src ? k : 1, E, d_model, d_ff);
   REQUIRE(ws_bytes >= need, LAEP_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", name, ws_bytes,
           need);
-  const size_t x_bytes = (size_t)T * d_model * 2, y_bytes = (size_t)R * d_model * 2;
-  const size_t a_bytes = (size_t)R * d_ff * 4;
-  const size_t gu_bytes = (size_t)d_ff * d_model, d_bytes = (size_t)d_ff * d_model / 2;
-  const struct {
-    const void* p;
-    size_t n;
-  } in[] = {{x, x_bytes}, {w_gate_up, gu_bytes}, {w_down, d_bytes}, {ws, need},
-            {w_gate_up_scale, mx4_scale_bytes(2 * (int64_t)d_ff, d_model)},
-            {w_down_scale, mx4_scale_bytes(d_model, d_ff)}};
-  for (const auto& b : in)
-    REQUIRE(!overlap(y_perm, y_bytes, b.p, b.n) && !overlap(act_save, a_bytes, b.p, b.n),
-            LAEP_ERR_INVALID_ARG, "%s: y_perm and act_save must not overlap the inputs or ws",
-            name);
-  REQUIRE(!overlap(y_perm, y_bytes, act_save, a_bytes), LAEP_ERR_INVALID_ARG,
-          "%s: y_perm must not overlap act_save", name);
+  const size_t slots = expert_map ? 1 : E;
+  rc = check_mx4_overlap(
+      name, "y_perm, act_save and ws",
+      {{y_perm, (size_t)R * d_model * 2}, {act_save, (size_t)R * d_ff * 4}, {ws, need}},
+      {{x, (size_t)T * d_model * 2},
+       {row_src, (size_t)R * 4},
+       {w_gate_up, slots * d_ff * d_model},
+       {w_gate_up_scale, slots * mx4_scale_bytes(2 * (int64_t)d_ff, d_model)},
+       {w_down, slots * d_ff * d_model / 2},
+       {w_down_scale, slots * mx4_scale_bytes(d_model, d_ff)},
+       {offsets, (size_t)(E + 1) * 4},
+       {expert_map, (size_t)E * 4}});
+  if (rc) return rc;
   return hip_status(laep::launch_ffn_fwd_mx4(x, row_src, T, k, w_gate_up, w_gate_up_scale, w_down,
                                              w_down_scale, offsets, expert_map, act_bits, E,
                                              d_model, d_ff, R, y_perm, act_save, ws,

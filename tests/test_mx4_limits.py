@@ -2,7 +2,7 @@
 import pytest
 
 import paper_2601_14327_amd as laep
-from test_abi import L, _err  # noqa: F401  (L: the library fixture)
+from test_abi import L, _err, _fake  # noqa: F401  (L: the library fixture)
 
 
 @pytest.mark.parametrize("R,f", [(1 << 28, 256), ((1 << 28) - 1, 320), (1 << 25, 2048)])
@@ -21,3 +21,55 @@ def test_no_tiles_where_the_ffn_refuses_the_rows(L, R, f):
                                          None, bits, E, d, f, R, None, None, None, 0, None)
     assert call(R, 4) == 2 and "too many" in _err(L)
     assert call(few, 4) == 1 and call(R, 16) == 1      # (no offsets)
+
+
+@pytest.fixture()
+def ptrs():
+    keep, p = _fake(65536)   # 4 MB
+    yield [p + 262144 * i for i in range(15)]
+    del keep
+
+
+def _alias_checks(f, L, outs, ins, with_map):
+    """No output or workspace over an input's first or last bytes."""
+    for o in outs:
+        for name, (p, n) in ins.items():
+            kw = dict(em=ins["em"][0]) if with_map or name == "em" else {}
+            for at in (p, p + max(n - 16, 0) // 16 * 16):
+                assert f(**{o: at}, **kw) == 1 and "overlap" in _err(L), (o, name, at - p)
+
+
+def test_product_buffers_that_overlap_are_refused(L, ptrs):
+    x, xs, src, w, wsc, off, em, out, ws = ptrs[:9]
+    T, k, E, N, K, R = 4, 2, 8, 64, 128, 8
+    need = L.moe_workspace_bytes(7, T, k, E, K, N)
+
+    def f(x=x, xs=xs, src=src, w=w, wsc=wsc, off=off, em=None, out=out, ws=ws):
+        return L.moe_mx4_grouped_product(x, xs, src, T, k, w, wsc, off, em, 1, E, N, K, R, out, ws,
+                                         need, None)
+
+    # without a map the weights are all E slots, with one the first is looked at
+    for slots in (E, 1):
+        _alias_checks(f, L, ("out", "ws"),
+                      dict(x=(x, T * K // 2), xs=(xs, T * 8), src=(src, 4 * R), off=(off, 4 * E + 4),
+                           em=(em, 4 * E), w=(w, slots * N * K // 2), wsc=(wsc, slots * N * 8)),
+                      slots == 1)
+    assert f(out=ws) == 1 and f(ws=out) == 1 and "overlap" in _err(L)
+    assert f(xs=None, out=x + 2 * T * K - 16) == 1 and f(xs=None, ws=x + 2 * T * K - 16) == 1
+
+
+def test_ffn_buffers_that_overlap_are_refused(L, ptrs):
+    x, src, wg, wgs, wd, wds, off, em, y, act, ws = ptrs[:11]
+    T, k, E, d, ff, R = 4, 2, 8, 128, 64, 8
+    need = L.moe_workspace_bytes(8, T, k, E, d, ff)
+
+    def f(em=None, y=y, act=act, ws=ws):
+        return L.moe_grouped_ffn_fwd_mx4(x, src, T, k, wg, wgs, wd, wds, off, em, 16, E, d, ff, R,
+                                         y, act, ws, need, None)
+
+    for slots in (E, 1):
+        _alias_checks(f, L, ("y", "act", "ws"),
+                      dict(x=(x, 2 * T * d), src=(src, 4 * R), off=(off, 4 * E + 4), em=(em, 4 * E),
+                           wg=(wg, slots * ff * d), wgs=(wgs, slots * 2 * ff * 8),
+                           wd=(wd, slots * ff * d // 2), wds=(wds, slots * d * 8)), slots == 1)
+    assert f(act=y) == 1 and f(y=ws) == 1 and f(act=ws + need - 16) == 1 and "overlap" in _err(L)
