@@ -855,6 +855,14 @@ def _need_mx4(w, name: str, lead, R: int, C: int, device):
         _need(scale, f"{name}.scale", lead + (-(-C // LAEP_MX4_GROUP), R, 8), u8, device)
 
 
+_INT_MAX = 0x7FFFFFFF   # (ctypes passes a larger number's low 32 bits as a C int)
+
+
+def _too_large(**sizes):
+    name, n = max(sizes.items(), key=lambda kv: kv[1])
+    raise ValueError(f"{name}={n} is past the C calls' 2^31 - 1")
+
+
 def _on_device(device, fn, *args):
     """check(fn(*args, stream)) with the tensors' device current: the C calls launch there."""
     index = device.index
@@ -873,11 +881,14 @@ def moe_mx4_quantize(src: torch.Tensor, *, codes=None, scale=None) -> Mx4:
     if len(shape) < 2:
         raise ValueError("src must have rows and columns")
     lead, R, C = shape[:-2], shape[-2], shape[-1]
+    n = math.prod(lead)
+    if n > _INT_MAX or C > _INT_MAX:
+        _too_large(matrices=n, columns=C)
     dev = src.device
     code = _dtype_code(src)
     codes = _need_out(codes, "codes", lead + (R, C // 2), torch.uint8, dev)
     scale = _need_out(scale, "scale", lead + (-(-C // LAEP_MX4_GROUP), R, 8), torch.uint8, dev)
-    _on_device(dev, lib().moe_mx4_quantize, src.data_ptr(), code, math.prod(lead), R, C,
+    _on_device(dev, lib().moe_mx4_quantize, src.data_ptr(), code, n, R, C,
                codes.data_ptr(), scale.data_ptr())
     return Mx4(codes, scale)
 
@@ -890,6 +901,9 @@ def moe_mx4_dequantize(codes: torch.Tensor, scale: torch.Tensor,
     if len(shape) < 2:
         raise ValueError("codes must have rows and columns")
     lead, R, C = shape[:-2], shape[-2], 2 * shape[-1]
+    n = math.prod(lead)
+    if n > _INT_MAX or C > _INT_MAX:
+        _too_large(matrices=n, columns=C)
     dev = codes.device
     if dtype not in _DT:
         raise LaepError(2, f"unsupported dtype {dtype}")
@@ -897,7 +911,7 @@ def moe_mx4_dequantize(codes: torch.Tensor, scale: torch.Tensor,
     _need(scale, "scale", lead + (-(-C // LAEP_MX4_GROUP), R, 8), torch.uint8, dev)
     out = _need_out(out, "out", lead + (R, C), dtype, dev)
     _on_device(dev, lib().moe_mx4_dequantize, codes.data_ptr(), scale.data_ptr(), _DT[dtype],
-               math.prod(lead), R, C, out.data_ptr())
+               n, R, C, out.data_ptr())
     return out
 
 
@@ -939,6 +953,9 @@ def moe_mx4_grouped_product(x, w: Mx4, offsets: torch.Tensor, *, row_src=None, k
     slots, N, _ = w[0].shape
     if mx4:
         K *= 2
+    if T > _INT_MAX or K > _INT_MAX or N > _INT_MAX or k > _INT_MAX:
+        _too_large(T=T, K=K, N=N, k=k)
+    if mx4:
         _need_mx4(x, "x", (), T, K, dev)
     else:
         _need(x, "x", (T, K), torch.bfloat16, dev)
@@ -973,6 +990,8 @@ def moe_grouped_ffn_fwd_mx4(x: torch.Tensor, w_gate_up: Mx4, w_down: Mx4,
     T, d = x.shape
     slots, _, f = w_down[0].shape
     f *= 2
+    if T > _INT_MAX or d > _INT_MAX or f > _INT_MAX or k > _INT_MAX:
+        _too_large(T=T, d=d, f=f, k=k)
     _need(x, "x", (T, d), torch.bfloat16, dev)
     _need_mx4(w_gate_up, "w_gate_up", (slots,), 2 * f, d, dev)
     _need_mx4(w_down, "w_down", (slots,), d, f, dev)

@@ -1,5 +1,6 @@
 """Limits of the calls at microscaled 4-bit weights, and what looks them up (host code)."""
 import pytest
+import torch
 
 import paper_2601_14327_amd as laep
 from test_abi import L, _err, _fake  # noqa: F401  (L: the library fixture)
@@ -73,3 +74,47 @@ def test_ffn_buffers_that_overlap_are_refused(L, ptrs):
                            wg=(wg, slots * ff * d), wgs=(wgs, slots * 2 * ff * 8),
                            wd=(wd, slots * ff * d // 2), wds=(wds, slots * d * 8)), slots == 1)
     assert f(act=y) == 1 and f(y=ws) == 1 and f(act=ws + need - 16) == 1 and "overlap" in _err(L)
+
+
+class _Huge:
+    """What the binding asks of a device tensor before it looks at its memory."""
+    is_cuda, device = True, torch.device("cuda", 0)
+
+    def __init__(self, *shape, dtype=torch.uint8):
+        self.shape, self.dtype = torch.Size(shape), dtype
+
+    def dim(self):
+        return len(self.shape)
+
+    def is_contiguous(self):
+        return True
+
+    def get_device(self):
+        return 0
+
+
+@pytest.mark.parametrize("n", [1 << 31, (1 << 32) + 64])
+def test_sizes_past_a_c_int_are_refused(n):
+    """(The C calls would be passed their low 32 bits: 64 columns of 2^32 + 64.)"""
+    bf16, off = torch.bfloat16, torch.zeros(2, dtype=torch.int32)
+
+    def w(N, K):
+        return laep.Mx4(_Huge(1, N, K // 2), _Huge(1, -(-K // 256), N, 8))
+
+    def x(T, K):
+        return _Huge(T, K, dtype=bf16)
+
+    for call in (lambda: laep.moe_mx4_quantize(x(1, n)),
+                 lambda: laep.moe_mx4_quantize(_Huge(n, 1, 32, dtype=bf16)),
+                 lambda: laep.moe_mx4_dequantize(_Huge(1, n // 2), _Huge(n // 256 + 1, 1, 8)),
+                 lambda: laep.moe_mx4_dequantize(_Huge(n, 1, 16), _Huge(n, 1, 1, 8)),
+                 lambda: laep.moe_mx4_grouped_product(x(n, 64), w(64, 64), off),
+                 lambda: laep.moe_mx4_grouped_product(x(8, n), w(64, n), off),
+                 lambda: laep.moe_mx4_grouped_product(x(8, 64), w(n, 64), off),
+                 lambda: laep.moe_mx4_grouped_product(x(8, 64), w(64, 64), off, k=n),
+                 lambda: laep.moe_grouped_ffn_fwd_mx4(x(n, 64), w(128, 64), w(64, 64), off),
+                 lambda: laep.moe_grouped_ffn_fwd_mx4(x(8, n), w(128, n), w(n, 64), off),
+                 lambda: laep.moe_grouped_ffn_fwd_mx4(x(8, 64), w(2 * n, 64), w(64, n), off),
+                 lambda: laep.moe_grouped_ffn_fwd_mx4(x(8, 64), w(128, 64), w(64, 64), off, k=n)):
+        with pytest.raises(ValueError, match=f"={n} is past"):
+            call()
