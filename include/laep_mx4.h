@@ -48,8 +48,9 @@ int moe_mx4_quantize(const void* src, int dtype, int n, int64_t R, int C,
 
 /*
  * moe_mx4_dequantize -- the values codes and scales stand for, in dtype (exact
- * in bf16 and float32); NaN where the scale is 255.  Arrays as in
- * moe_mx4_quantize.
+ * in bf16 and float32, but for scales that moe_mx4_quantize does not write: at
+ * b = 253 the steps 4 and 6, at b = 254 those from 2 up are infinities); NaN where
+ * the scale is 255.  Arrays as in moe_mx4_quantize.
  */
 int moe_mx4_dequantize(const uint8_t* codes, const uint8_t* scale, int dtype,
                        int n, int64_t R, int C, void* out, void* stream);
@@ -64,7 +65,8 @@ int moe_mx4_dequantize(const uint8_t* codes, const uint8_t* scale, int dtype,
  *   x        device [T, K]: MX4 codes with x_scale, or bf16 with x_scale NULL
  *   row_src  device [R] int32 (moe_expert_counts') or NULL (X's rows are
  *            already in the experts' order: T >= R, k unused)
- *   w, w_scale  device MX4 [slots, N, K]
+ *   w, w_scale  device MX4 [slots, N, K]; beside bf16 activations their values are
+ *            moe_mx4_dequantize's in bf16
  *   offsets  device [E + 1] int32; expert_map device [E] int32 or NULL (slot e);
  *            rows of experts with a negative slot, and rows outside every
  *            expert's range, are left as they were in out

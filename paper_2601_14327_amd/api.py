@@ -895,7 +895,8 @@ def moe_mx4_quantize(src: torch.Tensor, *, codes=None, scale=None) -> Mx4:
 
 def moe_mx4_dequantize(codes: torch.Tensor, scale: torch.Tensor,
                        dtype: torch.dtype = torch.bfloat16, *, out=None):
-    """The values [..., R, C] that codes and scale stand for, in dtype (exact)."""
+    """The values [..., R, C] that codes and scale stand for, in dtype (exact, if they are
+    moe_mx4_quantize's; infinities where a larger scale leaves float32's range)."""
     _dev(codes, "codes")
     shape = tuple(codes.shape)
     if len(shape) < 2:

@@ -9,7 +9,10 @@
 // in flight.  Rings in the LDS, and what a step is:
 //   MX4, 256 rows:   256 columns; three slots of A (32 KB), two of B, whose fragments are
 //                    all in registers after a quarter of the step.  Scales go to registers,
-//                    a dword per fragment and step, as the LDS is full.
+//                    a dword per fragment and step, as the LDS is full, in two sets.  The
+//                    compiler copies one of them at the loop's head, where every second
+//                    step so waits for scales that it loaded itself, and for the copies of
+//                    A before them.
 //   MX4, 128 rows:   256 columns; three slots of A (16 KB), of B and of scales.
 //   bf16, 256 rows:  64 columns; four slots of A (32 KB) and of weight codes (8 KB).
 //   bf16, 128 rows:  64 columns; five slots of A (16 KB), two of the codes and scales of four
@@ -22,10 +25,16 @@
 // their rows do: such tiles are dealt tallest first, forward and back (64 experts of 128
 // rows on average, 2048 x 2048, bf16: 95 -> 81 us).
 //
-// Measured on products of even experts: MX4 256 rows 3.3 PFLOP/s, the MFMA's power limit
-// with operands that come from the LDS being 5.9; bf16 256 rows 1.56 PFLOP/s at the margin
-// (a large library product: 1.60), 128 rows 1.36.  Where weights are hardly shared (up to
-// 128 rows an expert) the weights' stream bounds: 5 - 6 TB/s.
+// Measured on products of 64 even experts, 2048 x 2048, lists included: 256-row tiles of
+// 1024 and 2048 rows an expert in MX4 159 and 301 us (3.5 and 3.6 PFLOP/s), in bf16 417 and
+// 810 (1.32 and 1.36; a large library product: 1.60), with uneven experts the matrix cores
+// are busy 44 and 62 - 67 % of the cycles; 128-row tiles of 128 and 256 rows in MX4 35 and 48, in bf16 64 and 111
+// (1.08 and 1.24 PFLOP/s).  Where weights are hardly shared (up to 128 rows an expert) the
+// weights' stream bounds: 142 MB of codes and scales in MX4's 35 us.
+//
+// The 256-row bf16 SwiGLU kernel keeps 15 registers in scratch, some of them for the kept
+// pre-activations' path, and reloads them where the next tile's rows are read, where the
+// copies move on to it, and after a tile's stores: there it waits for everything in flight.
 #include <type_traits>
 
 #include "gemm_mx4.hpp"

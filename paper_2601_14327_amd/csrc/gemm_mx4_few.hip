@@ -1,18 +1,22 @@
 // Grouped products at MX4 weights for few rows an expert (decoding): the products of
 // gemm_mx4.hip in tiles of 32 rows x 64 weight rows.
 //
-// Every weight byte is used once, so the products are bound by streaming the weights, and
-// for a single token by the latency of one pass through them.  The waves of a workgroup
-// split K: wave w takes the 256-column steps w, w + 4, ..., 8 KB of codes each, which it
-// copies into LDS of its own; nothing waits for another wave until the partial sums are
-// added, in the waves' order.  Sixteen waves a CU, 128 KB in flight.  (us for gate/up and
-// down of 128 rows in 43 of 64 experts, d 2048, d_ff 1024, bf16 activations 18.4 + 11.2;
+// Every weight byte is used once, so the products are bound by streaming the weights.  A
+// single token has one workgroup a CU and is bound by latencies one after the other: the
+// offsets, row_src, and in each step first activations, whose loads the compiler puts ahead
+// of the weights' copies and waits for, then the copies; nothing of the next step is in
+// flight (gate/up, two steps a wave, 8.1 us for 18 MB; down, one step, 4.9 for 9 MB).
+// The waves of a workgroup split K: wave w takes the 256-column steps w, w + 4, ..., 8 KB
+// of codes each, which it copies into LDS of its own; nothing waits for another wave until
+// the partial sums are added, in the waves' order.  Sixteen waves a CU, 128 KB in flight.
+// (us for gate/up and down of 128 rows in 43 of 64 experts, d 2048, d_ff 1024, bf16 activations 19.0 + 10.9;
 // eight waves a tile 22.5 + 11.5; two steps in flight a wave and eight waves a CU 19.7 +
 // 13.6; a tile a wave, no sums to add, 23.8 + 13.1; weights streamed past the caches 20.4
 // + 11.9.)
 // Activations go from memory to registers; the FFN's X becomes MX4 there, so no launch
 // and no buffer stand between it and the first product.  No tile list: every wave finds
-// its tile from the expert offsets.
+// its tile from the expert offsets.  The bf16 gate/up kernel needs six registers more than
+// the 128 that sixteen waves a CU leave, and keeps them in scratch.
 #include "gemm_mx4.hpp"
 
 namespace laep {

@@ -4,7 +4,7 @@
 // HBM-bound.  A workgroup takes rows of one group of 256 columns, whose eight scale bytes
 // a row lie beside the next row's, so codes are written in whole 128-byte lines and
 // scales in whole runs of rows.  64 x 2048 x 1024 in bf16 (340 MB): 56 us quantised (6.0
-// TB/s), 48 us back (7.0, part of the codes still in the cache); 8 x 2048: 2.8 and 2.7 us.
+// TB/s), 48 us back (7.0, part of the codes still in the cache); 8 x 2048: 2.7 us each.
 #include "common.hpp"
 #include "internal.hpp"
 #include "mx4.hpp"
